@@ -6,6 +6,7 @@ used for device memory and streams only:
   X        : float16 [N, K] contiguous            (== column-major K x N, ld = K)
   C        : float16 [N, M] contiguous            (== column-major M x N, ld = M)
   blob     : uint8 1-D
+  Wq, Ws   : float8_e4m3fn [M, K], float8_e8m0fnu [M, scale_stride(K)], contiguous
 There is no CPU fallback: without the built library, or without a GPU, calls raise.
 """
 import ctypes
@@ -28,7 +29,8 @@ _lib = None
 _ws_tensor = None  # keeps the registered workspace alive
 
 EXPORTS = ("fls_compress_bound", "fls_compress", "fls_compress_bound_v2", "fls_compress_v2", "fls_inspect", "fls_workspace_bytes", "fls_set_workspace",
-           "fls_check_workspace", "fls_spmm", "fls_spmm_stats", "fls_spmm_noalloc", "fls_forget", "fls_dense_gemm", "fls_strerror")
+           "fls_check_workspace", "fls_spmm", "fls_spmm_stats", "fls_spmm_noalloc", "fls_forget", "fls_dense_gemm", "fls_quantize",
+           "fls_fp8_workspace_bytes", "fls_fp8_gemm", "fls_strerror")
 
 
 class FlsStats(ctypes.Structure):
@@ -97,6 +99,12 @@ def lib():
         L.fls_forget.restype = None
         L.fls_dense_gemm.argtypes = [vp, vp, vp, i64, i64, i64, vp]
         L.fls_dense_gemm.restype = ci
+        L.fls_quantize.argtypes = [vp, i64, i64, vp, vp, vp]
+        L.fls_quantize.restype = ci
+        L.fls_fp8_workspace_bytes.argtypes = [i64, i64, i64]
+        L.fls_fp8_workspace_bytes.restype = sz
+        L.fls_fp8_gemm.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp]
+        L.fls_fp8_gemm.restype = ci
         L.fls_internal_spmm_plan.argtypes = [ctypes.c_uint32] * 5 + [ci, ci, ctypes.POINTER(ctypes.c_uint32)]
         L.fls_internal_spmm_plan.restype = None
         L.fls_strerror.argtypes = [ci]
@@ -335,3 +343,71 @@ def fls_dense_gemm(W, X, C, M, K, N):
     _check(lib().fls_dense_gemm(W.data_ptr(), X.data_ptr(),
                                 C.data_ptr(), M, K, N, _stream()), "fls_dense_gemm")
     return C
+
+
+def scale_stride(K):
+    """Scales to a row of K quantised values: one for each 128, up to a multiple of four."""
+    return (K + 511) // 512 * 4
+
+
+def fls_quantize(W, out=None):
+    """W: float16 [M, K] CUDA tensor, K a multiple of 16.  Returns (Wq float8_e4m3fn [M, K], Ws float8_e8m0fnu [M, scale_stride(K)])."""
+    import torch
+
+    assert W.is_cuda and W.dtype == torch.float16 and W.is_contiguous() and W.dim() == 2
+    M, K = W.shape
+    if out is None:
+        out = (torch.empty((M, K), dtype=torch.float8_e4m3fn, device=W.device),
+               torch.empty((M, scale_stride(K)), dtype=torch.float8_e8m0fnu, device=W.device))
+    Wq, Ws = out
+    assert Wq.is_cuda and Wq.dtype == torch.float8_e4m3fn and Wq.is_contiguous() and Wq.shape == (M, K)
+    assert Ws.is_cuda and Ws.dtype == torch.float8_e8m0fnu and Ws.is_contiguous() and Ws.shape == (M, scale_stride(K))
+    _check(lib().fls_quantize(W.data_ptr(), M, K, Wq.data_ptr(), Ws.data_ptr(), _stream()), "fls_quantize")
+    return Wq, Ws
+
+
+def fls_fp8_workspace_bytes(M, K, N):
+    return int(lib().fls_fp8_workspace_bytes(M, K, N))
+
+
+def _ensure(need, where):
+    import torch
+
+    if need == 0:
+        raise FlsError(EINVAL, where)
+    if _ws_tensor is None or _ws_tensor.numel() < need:
+        fls_set_workspace(torch.empty(need, dtype=torch.uint8, device="cuda"))
+
+
+def ensure_fp8_workspace(M, K, N):
+    """ensure_workspace for fls_fp8_gemm."""
+    _ensure(fls_fp8_workspace_bytes(M, K, N), "fls_fp8_workspace_bytes")
+
+
+def _fp8_args(Wq, Ws, X, C, M, K, N):
+    import torch
+
+    assert Wq.is_cuda and Wq.dtype == torch.float8_e4m3fn and Wq.is_contiguous() and Wq.shape == (M, K)
+    assert Ws.is_cuda and Ws.dtype == torch.float8_e8m0fnu and Ws.is_contiguous() and Ws.shape == (M, scale_stride(K))
+    assert X.is_cuda and X.dtype == torch.float16 and X.is_contiguous() and X.shape == (N, K)
+    assert C.is_cuda and C.dtype == torch.float16 and C.is_contiguous() and C.shape == (N, M)
+    return Wq.data_ptr(), Ws.data_ptr(), X.data_ptr(), C.data_ptr(), M, K, N, _stream()
+
+
+def fls_fp8_gemm(Wq, Ws, X, C, M, K, N):
+    """C = W . X with W as fls_quantize returned it; X float16 [N, K], C float16 [N, M] as everywhere."""
+    _check(lib().fls_fp8_gemm(*_fp8_args(Wq, Ws, X, C, M, K, N)), "fls_fp8_gemm")
+    return C
+
+
+def prepare_fp8_gemm(Wq, Ws, X, C, M, K, N):
+    """As prepare_spmm, for fls_fp8_gemm."""
+    f, args = lib().fls_fp8_gemm, _fp8_args(Wq, Ws, X, C, M, K, N)
+    keep = (Wq, Ws, X, C)
+
+    def call(_keep=keep):
+        rc = f(*args)
+        if rc != OK:
+            _check(rc, "fls_fp8_gemm")
+
+    return call

@@ -556,6 +556,61 @@ int fls_dense_gemm(const void* W_dev, const void* X_dev, void* C_dev, int64_t M,
   return fls::launch_dense(a, (hipStream_t)stream) == hipSuccess ? FLS_OK : FLS_EHIP;
 }
 
+// Matrices of the 8-bit products: rows and k that the kernels' 32-bit offsets inside a tile of 256 rows reach.
+static bool fp8_shape_ok(int64_t M, int64_t K) { return M >= 1 && M <= FLS_FP8_MAX_M && K >= 16 && K <= FLS_FP8_MAX_K && K % 16 == 0; }
+
+// Workspace of fls_fp8_gemm: the control area, which it leaves alone, sums of K slices, X quantised and its scales.
+static bool fp8_layout(int64_t M, int64_t K, int64_t N, size_t* xq, size_t* xs, size_t* total) {
+  if (!fp8_shape_ok(M, K) || N < 1 || N > FLS_MAX_N) return false;
+  if ((uint64_t)K * (uint64_t)N * 2u > 0x7fffffffull || (uint64_t)M * (uint64_t)N * 2u > 0x7fffffffull) return false;
+  *xq = kCounterAreaBytes + fls::fp8_parts_bytes();
+  *xs = *xq + round_up((uint64_t)N * (uint64_t)K, 16);
+  *total = *xs + round_up((uint64_t)N * fls::scale_stride((uint32_t)K), 16);
+  return true;
+}
+
+int fls_quantize(const void* W_dev, int64_t M, int64_t K, void* Wq_dev, void* Ws_dev, fls_stream_t stream) {
+  if (!W_dev || !Wq_dev || !Ws_dev || !fp8_shape_ok(M, K)) return FLS_EINVAL;
+  if (!aligned16(W_dev) || !aligned16(Wq_dev) || !aligned16(Ws_dev)) return FLS_EALIGN;
+  return fls::launch_quantize((const _Float16*)W_dev, (uint8_t*)Wq_dev, (uint8_t*)Ws_dev, (uint64_t)M, (uint32_t)K, (hipStream_t)stream) == hipSuccess
+             ? FLS_OK
+             : FLS_EHIP;
+}
+
+size_t fls_fp8_workspace_bytes(int64_t M, int64_t K, int64_t N) {
+  size_t xq, xs, total;
+  return fp8_layout(M, K, N, &xq, &xs, &total) ? total : 0;
+}
+
+int fls_fp8_gemm(const void* Wq_dev, const void* Ws_dev, const void* X_dev, void* C_dev, int64_t M, int64_t K, int64_t N,
+                 fls_stream_t stream) {
+  if (!Wq_dev || !Ws_dev || !X_dev || !C_dev) return FLS_EINVAL;
+  size_t xq, xs, need;
+  if (!fp8_layout(M, K, N, &xq, &xs, &need)) return FLS_EINVAL;
+  if (!aligned16(Wq_dev) || !aligned16(Ws_dev) || !aligned16(X_dev) || !aligned16(C_dev)) return FLS_EALIGN;
+  unsigned char* ws;
+  {
+    std::lock_guard<std::mutex> lk(g_mu);
+    if (!g_ws || g_ws_bytes < need) return FLS_EWORKSPACE;
+    ws = (unsigned char*)g_ws;
+  }
+  const int cus = num_cus();
+  if (cus <= 0) return FLS_EHIP;
+  fls::Fp8Launch a;
+  a.W = (const uint8_t*)Wq_dev;
+  a.Ws = (const uint8_t*)Ws_dev;
+  a.X = (const _Float16*)X_dev;
+  a.C = (_Float16*)C_dev;
+  a.parts = (float*)(ws + kCounterAreaBytes);
+  a.Xq = ws + xq;
+  a.Xs = ws + xs;
+  a.M = (uint32_t)M;
+  a.K = (uint32_t)K;
+  a.N = (uint32_t)N;
+  a.num_cus = cus;
+  return fls::launch_fp8(a, (hipStream_t)stream) == hipSuccess ? FLS_OK : FLS_EHIP;
+}
+
 void fls_internal_spmm_plan(uint32_t max_tile_words, uint32_t version, uint32_t M, uint32_t K, uint32_t N, int cus, int wide32,
                             uint32_t* out) {
   const fls::SpmmPlan plan = fls::spmm_plan(max_tile_words, version, M / FLS_TILE_M, K / FLS_TILE_K, N, cus, wide32 != 0);

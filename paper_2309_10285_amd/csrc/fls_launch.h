@@ -394,6 +394,58 @@ hipError_t launch_fill_zero(void* p, size_t bytes, hipStream_t stream);
 // all control words of a hand-over but the error word
 hipError_t launch_lower_flags(uint32_t* flags, hipStream_t stream);
 
+// --- products in 8-bit floating point -----------------------------------------------------------------------------------------
+
+constexpr uint32_t kQuantizeRows = 64;  // rows to a row of the quantising kernel's grid: 64 lanes-to-a-row stay below 2^29
+
+// Scales to a row: one for each 128 k, up to a multiple of four.
+inline uint32_t scale_stride(uint32_t K) { return (K + 511u) / 512u * 4u; }
+// Room for the sums of K slices.
+constexpr size_t fp8_parts_bytes() { return (size_t)64 << 20; }
+
+enum { kFp8StreamQuant, kFp8Stream, kFp8Tile };
+struct Fp8Plan {
+  int pass;
+  uint32_t slices;
+};
+Fp8Plan fp8_plan(uint32_t M, uint32_t K, uint32_t N, int cus);
+
+struct Fp8Launch {
+  const uint8_t *W, *Ws;
+  const _Float16* X;
+  _Float16* C;
+  float* parts;       // fp8_parts_bytes()
+  uint8_t *Xq, *Xs;   // N x K and N x scale_stride(K) bytes, for X quantised
+  uint32_t M, K, N;
+  int num_cus;
+};
+hipError_t launch_quantize(const _Float16* W, uint8_t* q, uint8_t* s, uint64_t rows, uint32_t K, hipStream_t stream);
+hipError_t launch_fp8(const Fp8Launch& a, hipStream_t stream);
+
+// --- attention ----------------------------------------------------------------------------------------------------------------
+
+struct AttentionLaunch {
+  const _Float16 *Q, *K, *V;
+  _Float16* O;
+  float* lse;  // [heads][q_rows] or null
+  const int32_t *q_start, *k_start, *k_len;
+  int64_t q_rows, k_rows, q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
+  uint32_t sequences, heads, kv_heads, dim, max_q;
+  int64_t max_k;
+  float scale;
+  float* parts;
+  int num_cus;
+};
+// How a call is cut.
+struct AttentionPlan {
+  uint32_t few;        // 1: the kernel for few queries to a sequence
+  uint32_t chunk;      // keys to a workgroup, a multiple of 128; all of them where `chunks` is 1
+  uint32_t chunks;     // at most that many chunks to a sequence
+  size_t parts_bytes;
+};
+AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t max_q, int64_t max_k);
+hipError_t launch_attention(const AttentionLaunch& a, hipStream_t stream);
+
 }  // namespace fls
 
 // What fls_spmm (wide32 = 1) or fls_spmm_noalloc (wide32 = 0) runs for a blob of that longest tile and version on a GPU of
