@@ -280,6 +280,45 @@ size_t fls_fp8_workspace_bytes(int64_t M, int64_t K, int64_t N);
 int fls_fp8_gemm(const void* Wq_dev, const void* Ws_dev, const void* X_dev, void* C_dev, int64_t M, int64_t K, int64_t N,
                  fls_stream_t stream);
 
+/*
+ * Causal attention between the QKV product and the output projection: for sequence b and its i-th query, counted from 0,
+ *   O_i = sum_j exp(scale q_i . k_j - lse_i) v_j,   lse_i = log sum_j exp(scale q_i . k_j),   j = 0 ... i + k_len[b] - queries of b,
+ * so that the last query sees all keys.  Query head h reads key head h / (heads / kv_heads).  A query that sees no key has O = 0 and lse = -inf.
+ * Queries of all sequences lie one sequence after the other: those of b are rows q_start[b] ... q_start[b + 1] - 1 of Q and O.  Its keys and
+ * values are rows k_start[b] ... k_start[b] + k_len[b] - 1 of K and V: the same rows of the QKV product's C for a prompt, a slab of a
+ * cache for a chunk of a prompt or a single token behind a stored prefix.  Rows of O and lse of no sequence stay as they were.
+ *
+ * All of Q, K, V, O are fp16; value d of head h of row r lies at [r * row + h * head + d], strides in elements.  Scores, their statistics and the
+ * sums are fp32; the weights exp(...) are rounded to fp16 for the product with V, O once.
+ */
+typedef struct {
+  int64_t q_rows;              /* rows of Q, O and of each head of lse */
+  int64_t k_rows;              /* rows of K and V, less than 2^31, as q_rows */
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head; /* strides: multiples of 8, rows of at most 2^22 */
+  int32_t sequences, heads, kv_heads; /* kv_heads divides heads */
+  int32_t head_dim;            /* a multiple of 8, at most FLS_MAX_HEAD_DIM */
+  int64_t max_q, max_k;        /* no sequence has more queries or keys; what one has beyond is not looked at */
+  float scale;                 /* positive and finite */
+} fls_attention_shape;
+
+#define FLS_MAX_HEAD_DIM 128
+
+/* Bytes of device workspace fls_attention needs for this shape: the control area of fls_workspace_bytes and, where a sequence's keys are
+ * shared out among workgroups because there are few queries, their sums.  Returns 0 on invalid arguments. */
+size_t fls_attention_workspace_bytes(const fls_attention_shape* shape_host);
+
+/*
+ *   q_start_dev in: int32, sequences + 1 values that do not decrease; k_start_dev, k_len_dev in: int32, `sequences` values each
+ *   lse_dev    out: fp32 [heads][q_rows], natural logarithms; may be NULL
+ *   shape_host  in: read during the call only
+ * Uses the registered workspace; enqueues kernels only, so it may be recorded into a HIP graph and replayed with other lengths, as long as
+ * max_q and max_k hold.  The lengths are read on the device: a sequence that lies outside 0 ... q_rows has no queries there, keys
+ * outside 0 ... k_rows are left out.  Keys that a query does not see do not touch it, be they infinite or NaN.  O may not overlap Q, K or V.
+ * The same call gives the same bits every time.  Errors: FLS_EINVAL, FLS_EALIGN, FLS_EWORKSPACE, FLS_EHIP.
+ */
+int fls_attention(const void* Q_dev, const void* K_dev, const void* V_dev, void* O_dev, float* lse_dev, const int32_t* q_start_dev,
+                  const int32_t* k_start_dev, const int32_t* k_len_dev, const fls_attention_shape* shape_host, fls_stream_t stream);
+
 /* Static description of an error code. */
 const char* fls_strerror(int code);
 

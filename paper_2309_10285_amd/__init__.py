@@ -30,7 +30,7 @@ _ws_tensor = None  # keeps the registered workspace alive
 
 EXPORTS = ("fls_compress_bound", "fls_compress", "fls_compress_bound_v2", "fls_compress_v2", "fls_inspect", "fls_workspace_bytes", "fls_set_workspace",
            "fls_check_workspace", "fls_spmm", "fls_spmm_stats", "fls_spmm_noalloc", "fls_forget", "fls_dense_gemm", "fls_quantize",
-           "fls_fp8_workspace_bytes", "fls_fp8_gemm", "fls_strerror")
+           "fls_fp8_workspace_bytes", "fls_fp8_gemm", "fls_attention_workspace_bytes", "fls_attention", "fls_strerror")
 
 
 class FlsStats(ctypes.Structure):
@@ -105,6 +105,10 @@ def lib():
         L.fls_fp8_workspace_bytes.restype = sz
         L.fls_fp8_gemm.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp]
         L.fls_fp8_gemm.restype = ci
+        L.fls_attention_workspace_bytes.argtypes = [vp]
+        L.fls_attention_workspace_bytes.restype = sz
+        L.fls_attention.argtypes = [vp] * 10
+        L.fls_attention.restype = ci
         L.fls_internal_spmm_plan.argtypes = [ctypes.c_uint32] * 5 + [ci, ci, ctypes.POINTER(ctypes.c_uint32)]
         L.fls_internal_spmm_plan.restype = None
         L.fls_strerror.argtypes = [ci]
@@ -409,5 +413,66 @@ def prepare_fp8_gemm(Wq, Ws, X, C, M, K, N):
         rc = f(*args)
         if rc != OK:
             _check(rc, "fls_fp8_gemm")
+
+    return call
+
+
+_ATTENTION_LAYOUT = struct.Struct("<10q4i2qf4x")  # fls_attention_shape
+
+
+def _attention_shape(Q, K, V, O, sequences, max_q, max_k, scale):
+    (q_rows, heads, dim), (k_rows, kv_heads, _) = Q.shape, K.shape
+    q, k, v, o = Q.stride(), K.stride(), V.stride(), O.stride()
+    q0, k0, v0, o0 = (q[0], k[0], v[0], o[0]) if q_rows > 1 and k_rows > 1 else (  # the stride of one row or head says nothing
+        q_rows > 1 and q[0], k_rows > 1 and k[0], k_rows > 1 and v[0], q_rows > 1 and o[0])
+    q1, o1 = (q[1], o[1]) if heads > 1 else (0, 0)
+    k1, v1 = (k[1], v[1]) if kv_heads > 1 else (0, 0)
+    return _ATTENTION_LAYOUT.pack(q_rows, k_rows, q0, q1, k0, k1, v0, v1, o0, o1, sequences, heads, kv_heads, dim, max_q, max_k, scale)
+
+
+def fls_attention_workspace_bytes(Q, K, sequences, max_q, max_k):
+    (q_rows, heads, dim), (k_rows, kv_heads, _) = Q.shape, K.shape  # strides do not matter here
+    return int(lib().fls_attention_workspace_bytes(_ATTENTION_LAYOUT.pack(q_rows, k_rows, 0, 0, 0, 0, 0, 0, heads * dim, dim, sequences, heads, kv_heads, dim,
+                                                                          max_q, max_k, 1.0)))
+
+
+def ensure_attention_workspace(Q, K, q_start, max_q, max_k):
+    """ensure_workspace for fls_attention."""
+    _ensure(fls_attention_workspace_bytes(Q, K, q_start.shape[0] - 1, max_q, max_k), "fls_attention_workspace_bytes")
+
+
+def _attention_args(Q, K, V, O, q_start, k_start, k_len, max_q, max_k, scale, lse):
+    import torch
+
+    f16, i32 = torch.float16, torch.int32
+    assert Q.is_cuda and Q.dtype == f16 and Q.dim() == 3 and Q.stride(2) == 1 and K.is_cuda and K.dtype == f16 and K.dim() == 3 and K.stride(2) == 1
+    assert V.is_cuda and V.dtype == f16 and V.shape == K.shape and V.stride(2) == 1 and O.is_cuda and O.dtype == f16 and O.shape == Q.shape and O.stride(2) == 1
+    assert K.shape[2] == Q.shape[2]
+    assert q_start.is_cuda and q_start.dtype == i32 and q_start.dim() == 1 and q_start.is_contiguous() and q_start.shape[0] > 0
+    sequences = q_start.shape[0] - 1
+    assert k_start.is_cuda and k_start.dtype == i32 and k_start.shape == (sequences,) and k_start.is_contiguous()
+    assert k_len.is_cuda and k_len.dtype == i32 and k_len.shape == (sequences,) and k_len.is_contiguous()
+    assert lse is None or (lse.is_cuda and lse.dtype == torch.float32 and lse.shape == (Q.shape[1], Q.shape[0]) and lse.is_contiguous())
+    return (Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), None if lse is None else lse.data_ptr(), q_start.data_ptr(), k_start.data_ptr(),
+            k_len.data_ptr(), _attention_shape(Q, K, V, O, sequences, max_q, max_k, scale), _stream())
+
+
+def fls_attention(Q, K, V, O, q_start, k_start, k_len, max_q, max_k, scale, lse=None):
+    """Causal attention of packed sequences: Q, O float16 [rows, heads, head_dim], K, V float16 [rows, kv_heads, head_dim], any strides but a last
+    one of 1 - slices of the QKV product's C, a cache.  q_start int32 [sequences + 1], k_start and k_len int32 [sequences], on the GPU: sequence b has
+    queries q_start[b] ... q_start[b + 1] - 1 and k_len[b] keys from row k_start[b] on, its last query sees all of them.  lse: float32 [heads, rows] or None."""
+    _check(lib().fls_attention(*_attention_args(Q, K, V, O, q_start, k_start, k_len, max_q, max_k, scale, lse)), "fls_attention")
+    return O
+
+
+def prepare_attention(Q, K, V, O, q_start, k_start, k_len, max_q, max_k, scale, lse=None):
+    """As prepare_spmm, for fls_attention; the lengths are read when the call runs."""
+    f, args = lib().fls_attention, _attention_args(Q, K, V, O, q_start, k_start, k_len, max_q, max_k, scale, lse)
+    keep = (Q, K, V, O, q_start, k_start, k_len, lse)
+
+    def call(_keep=keep):
+        rc = f(*args)
+        if rc != OK:
+            _check(rc, "fls_attention")
 
     return call

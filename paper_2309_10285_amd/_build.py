@@ -5,7 +5,7 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libfls.so")
-SOURCES = ["fls_api.hip", "fls_spmm.hip", "fls_spmm_wide.hip", "fls_spmm_block.hip", "fls_dense.hip", "fls_compress.hip", "fls_fp8.hip"]
+SOURCES = ["fls_api.hip", "fls_spmm.hip", "fls_spmm_wide.hip", "fls_spmm_block.hip", "fls_dense.hip", "fls_compress.hip", "fls_fp8.hip", "fls_attention.hip"]
 # measurement code (a plain streaming read: bench.py's empirical ceiling), a library of its own, not part of the C ABI
 PROBE_SOURCE = "fls_stream_probe.hip"
 PROBE_LIB = os.path.join(_HERE, "libfls_probe.so")

@@ -1,0 +1,584 @@
+// fls_attention: causal softmax attention with grouped heads over packed sequences, in one pass over the keys.
+//
+//   s_ij = scale q_i . k_j for j <= i + keys - queries,   o_i = sum_j exp(s_ij) v_j / sum_j exp(s_ij)
+//
+// A query keeps the largest score so far m (times log2 e: powers of two are what the hardware computes), the sum l of 2^(s - m) and
+// the sum o of 2^(s - m) v; when m grows, l and o are multiplied by 2^(old - new).  All three are fp32; 2^(s - m) is rounded to fp16
+// for the product with v (to nearest, 2^-11 of it), raised by 2^kLift so that what is small beside the largest is not subnormal.
+//
+// Both products are computed transposed, with 32x32x16 MFMAs: S^T = K Q^T gives lane l the column of query l & 31 and of 32 keys the rows
+// 8 a + 4 (l >> 5) + b (a, b = 0 ... 3), so that the largest and the sum of a query's scores are found inside a lane and
+// its neighbour 32 further.  In O^T = V^T P^T the same registers are the operand as they are: a lane's eight k may be any eight keys of 16, if
+// V^T has the same, and those are read from row-major V in LDS by transposing reads of four keys (ds_read_b64_tr_b16).
+//
+// Keys and values go to LDS without passing through registers.  16-byte piece c of row r lies at place c ^ turn(r), so that
+// eight lanes that read the same piece of eight rows find them in eight places, and the four rows of a transposing read as well.
+#include "fls_device.h"
+#include "fls_launch.h"
+
+namespace fls {
+
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+constexpr int kLift = 12;
+constexpr uint32_t kNowhere = 0x80000000u;  // an offset past every buffer descriptor here: a load from it gives 0
+constexpr float kInf = __builtin_inff();
+
+struct AttentionParams {
+  const _Float16 *Q, *K, *V;
+  _Float16* O;
+  float* lse;
+  const int32_t *q_start, *k_start, *k_len;
+  int64_t q_rows, k_rows, q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
+  uint32_t sequences, heads, rep, dim, max_q, max_k;
+  uint32_t chunk, chunks;     // keys to a workgroup where they are split, and into how many at most
+  uint32_t slots, units, row_blocks;
+  float scale_log2;           // scale * log2 e
+  float* part_o;              // [chunk][part row][head][DP] sums not yet divided; part rows: max_q to a sequence where there are few, else those of Q
+  float* part_ml;             // [chunk][part row][head][2]
+  uint64_t part_rows;
+  uint32_t few;
+  Divisor by_rep, by_chunks, by_row_blocks, by_kv_heads, by_slots;
+};
+
+// A sequence, cut to the tensors it lies in: whatever the arrays hold, nothing outside is read or written.
+struct Sequence {
+  int64_t q0, k0;
+  uint32_t nq, nk;
+};
+
+__device__ __forceinline__ Sequence sequence(const AttentionParams& p, uint32_t b) {
+  const int64_t a = p.q_start[b], e = p.q_start[b + 1], k = p.k_start[b], n = p.k_len[b];
+  Sequence s = {a, k, 0u, 0u};
+  if (a >= 0 && e > a && e <= p.q_rows) s.nq = (uint32_t)(e - a);
+  if (k >= 0 && n > 0 && k < p.k_rows) s.nk = (uint32_t)(n < p.k_rows - k ? n : p.k_rows - k);
+  s.nq = min(s.nq, p.max_q);
+  s.nk = min(s.nk, p.max_k);
+  return s;
+}
+
+template <int DP>
+__device__ __forceinline__ uint32_t turn(uint32_t row) {
+  return DP == 128 ? ((row & 7u) << 1 | (row >> 3 & 1u)) : ((row & 3u) << 1 | (row >> 2 & 1u));
+}
+
+// Where an array lies in LDS.
+__device__ __forceinline__ uint32_t lds_at(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
+
+// 16 bytes to a lane straight to LDS at `lds` + 16 lane (`lds` the same for the wave).  An asm statement, because the compiler waits for all loads into LDS
+// before it reads LDS with a transposing read, which would leave nothing in flight.  It writes no register but m0, which nothing else in these kernels
+// uses (the compiler keeps nothing there); who reads the LDS waits for it (vmcnt).
+__device__ __forceinline__ void load_lds(u32x4 buf, uint32_t lds, uint32_t off) {
+  const uint32_t at = __builtin_amdgcn_readfirstlane(lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(buf) : "memory");
+}
+
+// ROWS rows of DP values to LDS by THREADS lanes; rows from `left` on and values from dim on are 0.
+template <int DP, int ROWS, int THREADS>
+__device__ __forceinline__ void stage(const _Float16* first, int64_t row_stride, uint32_t left, uint32_t dim, uint32_t lds, uint32_t thread) {
+  constexpr uint32_t kPieces = DP / 8, kStep = THREADS / kPieces;  // rows to a load of all lanes
+  static_assert(ROWS % kStep == 0 && (kStep % 16 == 0 || 16 % kStep == 0), "whole loads");
+  const uint32_t bytes = left == 0u ? 0u : (uint32_t)((min(left, (uint32_t)ROWS) - 1u) * row_stride * 2 + dim * 2u);
+  const uint64_t base = (uint64_t)first;
+  const u32x4 buf = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, bytes, (uint32_t)kBufferFlags};  // raw buffer of `bytes` from `first` on
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+#pragma unroll
+  for (int i = 0; i < ROWS / (int)kStep; ++i) {
+    const uint32_t row = i * kStep + thread / kPieces, piece = (thread % kPieces) ^ turn<DP>(row);
+    const uint32_t off = row * (uint32_t)(row_stride * 2) + piece * 16u;
+    load_lds(buf, lds + i * THREADS * 16 + wave * 1024u, row < left && piece * 8u < dim ? off : kNowhere);
+  }
+}
+
+// What a wave knows of its 32 queries: lane l of query l & 31.
+template <int DP>
+struct Wave {
+  half8 q[DP / 16];
+  float16v o[DP / 32];
+  float m, l;
+  int limit;  // last key the query sees, from the first key of the sequence on; below 0: none
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) o[d] = float16v{};
+    m = -kInf;
+    l = 0.f;
+  }
+
+  // `here`: whether this lane's query is one
+  __device__ __forceinline__ void load(const _Float16* row, bool here, uint32_t dim, uint32_t lane) {
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) {
+      const uint32_t d = i * 16u + (lane >> 5) * 8u;
+      q[i] = half8{};
+      if (here && d < dim) q[i] = *(const half8*)(row + d);
+    }
+  }
+};
+
+__device__ __forceinline__ float across(float x, bool add) {  // with the lane 32 further
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t lower = r[0], upper = r[1];  // of r[1] itself, __builtin_bit_cast takes r[0]
+  const float a = __builtin_bit_cast(float, lower), b = __builtin_bit_cast(float, upper);
+  return add ? a + b : fmaxf(a, b);
+}
+
+// S^T of 32 keys, whose rows of K begin at `tile`.
+template <int DP>
+__device__ __forceinline__ float16v scores(const Wave<DP>& w, const uint8_t* tile, uint32_t lane) {
+  float16v s = {};
+  const uint8_t* row = tile + (lane & 31u) * (DP * 2);
+  const uint32_t t = turn<DP>(lane & 31u) ^ (lane >> 5);
+#pragma unroll
+  for (int i = 0; i < DP / 16; ++i) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)(row + ((2u * i ^ t) << 4)), w.q[i], s, 0, 0, 0);
+  return s;
+}
+
+// Eight keys of V^T for 32 d: keys key + 4 (l >> 5) + 0 ... 3 and the same 8 further, as S^T has them.
+template <int DP>
+__device__ __forceinline__ half8 values(const uint8_t* tile, uint32_t key, uint32_t d, uint32_t lane) {
+  const uint32_t row = key + 4u * (lane >> 5) + ((lane & 15u) >> 2), piece = d / 8u + 2u * ((lane >> 4) & 1u) + ((lane & 3u) >> 1);
+  typedef __attribute__((address_space(3))) short4v* lds_ptr;
+  const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + row * (DP * 2) + ((piece ^ turn<DP>(row)) << 4) + (lane & 1u) * 8u));
+  const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + (row + 8u) * (DP * 2) + ((piece ^ turn<DP>(row + 8u)) << 4) + (lane & 1u) * 8u));
+  return __builtin_bit_cast(half8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Key of score i of a lane.
+__device__ __forceinline__ uint32_t key_of(int i, uint32_t lane) { return 8u * (i / 4) + 4u * (lane >> 5) + i % 4; }
+
+// Weights of 32 B keys from their scores: m, l and o are brought up to date, s becomes 2^(s - m + kLift).
+template <int DP, int B>
+__device__ __forceinline__ void soften(Wave<DP>& w, float16v (&s)[B], float scale_log2) {
+  float top = s[0][0];
+#pragma unroll
+  for (int b = 0; b < B; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+  const float m = fmaxf(w.m, across(top, false) * scale_log2);
+  const float base = m == -kInf ? 0.f : m - kLift;  // a query that has seen no key: its weights are 0, not NaN
+  const float down = __builtin_amdgcn_exp2f(w.m - (base + kLift));
+  w.m = m;
+  float sum = 0.f;
+#pragma unroll
+  for (int b = 0; b < B; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale_log2, -base));
+      sum += s[b][i];
+    }
+  w.l = w.l * down + sum;  // of this lane's keys; both lanes' in the end
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w.o[d][i] *= down;
+}
+
+__device__ __forceinline__ half8 weights(const float16v& s, int half) {
+  half8 r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = (_Float16)s[half * 8 + i];
+  return r;
+}
+
+template <int DP, int B>
+__device__ __forceinline__ void add_values(Wave<DP>& w, const float16v (&s)[B], const uint8_t* tile, uint32_t lane) {
+#pragma unroll
+  for (int k = 0; k < 2 * B; ++k) {
+    const half8 p = weights(s[k / 2], k & 1);
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) w.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(values<DP>(tile, k * 16u, d * 32u, lane), p, w.o[d], 0, 0, 0);
+  }
+}
+
+// Does V in LDS hold an infinity or NaN?
+template <int DP, int ROWS>
+__device__ __forceinline__ bool any_not_finite(const uint8_t* tile, uint32_t lane) {
+  bool found = false;
+#pragma unroll
+  for (int i = 0; i < ROWS * DP / 512; ++i) {
+    const half8 v = *(const half8*)(tile + (i * 64u + lane) * 16u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) found |= !(__builtin_fabsf16(v[e]) <= (_Float16)65504.f);
+  }
+  return __any(found);
+}
+
+// add_values where some queries do not see some keys whose values are not finite: a weight of 0 times those is NaN.  Query by query,
+// with the values that the query does not see taken as 0; 32 times the work, for tiles that any_not_finite finds.
+template <int DP, int B>
+__device__ __forceinline__ void add_seen_values(Wave<DP>& w, const float16v (&s)[B], const uint8_t* tile, int key0, uint32_t lane) {
+  half8 p[2 * B];
+#pragma unroll
+  for (int k = 0; k < 2 * B; ++k) p[k] = weights(s[k / 2], k & 1);
+#pragma unroll 1
+  for (uint32_t query = 0; query < 32u; ++query) {
+    const int limit = __builtin_amdgcn_readlane(w.limit, query) - key0;
+    const bool mine = (lane & 31u) == query;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) {
+      float16v o = {};
+#pragma unroll
+      for (int k = 0; k < 2 * B; ++k) {
+        half8 v = values<DP>(tile, k * 16u, d * 32u, lane);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if ((int)(k / 2 * 32u + key_of((k & 1) * 8 + i, lane)) > limit) v[i] = (_Float16)0.f;
+        o = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[k], o, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w.o[d][i] = mine ? w.o[d][i] + o[i] : w.o[d][i];
+    }
+  }
+}
+
+// One tile of 32 B keys from key0 on (relative to the sequence), of which `nk` is the number of keys.
+template <int DP, int B, bool MASK>
+__device__ __forceinline__ void attend(Wave<DP>& w, const uint8_t* k_tile, const uint8_t* v_tile, int key0, float scale_log2, uint32_t lane) {
+  float16v s[B];
+#pragma unroll
+  for (int b = 0; b < B; ++b) {
+    s[b] = scores<DP>(w, k_tile + b * 32 * DP * 2, lane);
+    if (MASK) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (key0 + (int)(b * 32u + key_of(i, lane)) > w.limit) s[b][i] = -kInf;
+    }
+  }
+  soften<DP, B>(w, s, scale_log2);
+  if (MASK && any_not_finite<DP, 32 * B>(v_tile, lane)) add_seen_values<DP, B>(w, s, v_tile, key0, lane);
+  else add_values<DP, B>(w, s, v_tile, lane);
+}
+
+// 32 d of a lane's query: four in a row at 8 a + 4 (l >> 5)
+template <int DP>
+__device__ __forceinline__ void store_rows(const Wave<DP>& w, _Float16* row, float factor, uint32_t dim, uint32_t lane) {
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      const uint32_t at = d * 32u + a * 8u + (lane >> 5) * 4u;
+      if (at < dim)
+        *(half4*)(row + at) = half4{(_Float16)(w.o[d][4 * a] * factor), (_Float16)(w.o[d][4 * a + 1] * factor), (_Float16)(w.o[d][4 * a + 2] * factor),
+                                    (_Float16)(w.o[d][4 * a + 3] * factor)};
+    }
+}
+
+__device__ __forceinline__ float log_sum(float m, float l) { return l > 0.f ? (m - kLift + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : l == 0.f ? -kInf : l; }
+
+// --- many queries to a sequence ------------------------------------------------------------------------------------------------
+// A workgroup has 128 queries of a head, 32 to a wave; tiles of 64 keys go through LDS in two stages.  Tiles that every query sees
+// come first, in a loop without a mask.
+
+constexpr uint32_t kTileQ = 128, kTileKeys = 64;
+
+template <int DP>
+__global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
+  constexpr int kBytes = kTileKeys * DP * 2;
+  __shared__ __align__(16) uint8_t stages[2][2 * kBytes];  // a tile of K, one of V
+  const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t unit;
+  if (!xcd_unit(p.units, unit)) return;
+  // head by head, so that what runs at one time on an XCD reads the same keys; the last queries, which see the most keys, first
+  const uint32_t whole = divide(unit, p.by_chunks), c = unit - whole * p.chunks;
+  const uint32_t head = divide(whole, p.by_slots), slot = p.slots - 1u - (whole - head * p.slots);
+  // sequence b has the slots from q_start[b] / 128 + b on: at least one for each 128 of its queries
+  uint32_t b = 0;
+  for (uint32_t at = 0; at < p.sequences; at += 64u) {
+    const uint32_t i = at + lane;
+    const bool begun = i < p.sequences && (uint32_t)p.q_start[i] / kTileQ + i <= slot;
+    b += __popcll(__ballot(begun));
+  }
+  if (b == 0u) return;
+  --b;
+  const Sequence s = sequence(p, b);
+  const uint32_t first = (slot - ((uint32_t)p.q_start[b] / kTileQ + b)) * kTileQ;
+  if (first >= s.nq) return;
+  const int off = (int)s.nk - (int)s.nq;  // query i sees keys up to i + off
+
+  Wave<DP> w;
+  const uint32_t mine = first + wave * 32u + (lane & 31u);
+  const bool here = mine < s.nq;
+  const uint32_t g = divide(head, p.by_rep);
+  w.limit = here ? (int)mine + off : -1;
+  w.clear();
+
+  const int last = (int)min(first + kTileQ, s.nq) - 1 + off;  // last key that the workgroup's last query sees,
+  const int low = (int)first + off;                           // its first query,
+  const int high = min((int)(first + wave * 32u) + 31, (int)s.nq - 1) + off;  // the wave's last query
+  const uint32_t keys = last < 0 ? 0u : (uint32_t)last + 1u;
+  uint32_t t0 = 0, t1 = (keys + kTileKeys - 1) / kTileKeys;
+  if (p.chunks > 1u) {
+    if (c * (uint64_t)p.chunk >= s.nk) return;  // no such chunk
+    t0 = c * (p.chunk / kTileKeys);
+    t1 = min(t1, t0 + p.chunk / kTileKeys);
+  }
+  const uint32_t full = low < 0 ? 0u : ((uint32_t)low + 1u) / kTileKeys;  // tiles that all see
+  auto issue = [&](uint32_t t, uint32_t to) {
+    const int64_t row = s.k0 + (int64_t)t * kTileKeys;
+    const uint32_t left = s.nk - t * kTileKeys;
+    stage<DP, kTileKeys, 256>(p.K + row * p.k_row + (int64_t)g * p.k_head, p.k_row, left, p.dim, to, threadIdx.x);
+    stage<DP, kTileKeys, 256>(p.V + row * p.v_row + (int64_t)g * p.v_head, p.v_row, left, p.dim, to + kBytes, threadIdx.x);
+  };
+  uint32_t t = t0, now = 0;
+  const uint32_t lds = lds_at(stages);
+  auto begin = [&]() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's pieces of the tile are in LDS
+    __syncthreads();                                  // everybody's are, and nobody reads the other stage any more
+    if (t + 1u < t1) issue(t + 1u, lds + (now ^ 1u) * 2u * kBytes);
+  };
+  if (t < t1) issue(t, lds);
+  w.load(p.Q + (s.q0 + mine) * p.q_row + (int64_t)head * p.q_head, here, p.dim, lane);
+  __builtin_amdgcn_s_waitcnt(0);  // the compiler's loads have come: it has nothing to wait for among the loop's
+  for (; t < min(full, t1); ++t, now ^= 1u) {
+    begin();
+    attend<DP, 2, false>(w, stages[now], stages[now] + kBytes, (int)(t * kTileKeys), p.scale_log2, lane);
+  }
+  for (; t < t1; ++t, now ^= 1u) {
+    begin();
+#pragma unroll 1
+    for (uint32_t half = 0; half < 2u; ++half) {  // half a tile at a time: with a mask, a whole one needs more registers than there are
+      const int key0 = (int)(t * kTileKeys + half * 32u);
+      if (key0 <= high) attend<DP, 1, true>(w, stages[now] + half * 32u * DP * 2, stages[now] + kBytes + half * 32u * DP * 2, key0, p.scale_log2, lane);
+    }
+  }
+  w.l = across(w.l, true);
+  if (!here) return;
+  const int64_t row = s.q0 + mine;
+  if (p.chunks == 1u) {
+    store_rows<DP>(w, p.O + row * p.o_row + (int64_t)head * p.o_head, w.l > 0.f ? 1.f / w.l : w.l, p.dim, lane);
+    if (p.lse && lane < 32u) p.lse[(int64_t)head * p.q_rows + row] = log_sum(w.m, w.l);
+    return;
+  }
+  const uint64_t at = ((uint64_t)c * p.part_rows + row) * p.heads + head;
+  float* out = p.part_o + at * DP;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+      *(float4v*)(out + d * 32 + a * 8 + (lane >> 5) * 4u) = float4v{w.o[d][4 * a], w.o[d][4 * a + 1], w.o[d][4 * a + 2], w.o[d][4 * a + 3]};
+  if (lane < 32u) {
+    p.part_ml[at * 2] = w.m;
+    p.part_ml[at * 2 + 1] = w.l;
+  }
+}
+
+// --- few queries to a sequence -------------------------------------------------------------------------------------------------
+// Bound by the stream of keys and values.  The queries of all heads that share a key head are the 32 columns of a wave; a workgroup has
+// a chunk of a sequence's keys, its waves take tiles of 32 in turn, each with two stages of its own in LDS and no barrier, and add
+// up what they have at the end.
+
+constexpr uint32_t kFewWaves = 2, kFewKeys = 32;
+
+template <int DP>
+__global__ __launch_bounds__(kFewWaves * 64) void attention_few_kernel(AttentionParams p) {
+  constexpr int kBytes = kFewKeys * DP * 2;
+  __shared__ __align__(16) uint8_t stage0[kFewWaves][2 * kBytes], stage1[kFewWaves][2 * kBytes];
+  __shared__ float top[kFewWaves][32], sum[kFewWaves][32];
+  const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // chunk outermost: sequences of one length run side by side
+  const uint32_t kv_heads = p.heads / p.rep;
+  uint32_t u = blockIdx.x;
+  const uint32_t x = divide(u, p.by_row_blocks), block = u - x * p.row_blocks;
+  const uint32_t y = divide(x, p.by_kv_heads), g = x - y * kv_heads;
+  const uint32_t b = divide(y, p.by_chunks), c = y - b * p.chunks;
+  const Sequence s = sequence(p, b);
+  const uint32_t rows = s.nq * p.rep;
+  if (block * 32u >= rows) return;
+  const uint32_t begin = p.chunks > 1u ? c * p.chunk : 0u;
+  if (p.chunks > 1u && begin >= s.nk) return;  // no such chunk
+  const uint32_t end = p.chunks > 1u ? min(s.nk, begin + p.chunk) : s.nk;
+  const int off = (int)s.nk - (int)s.nq;
+
+  Wave<DP> w;
+  const uint32_t packed = block * 32u + (lane & 31u), query = divide(packed, p.by_rep), head = g * p.rep + packed - query * p.rep;
+  const bool here = packed < rows;
+  w.load(p.Q + (s.q0 + query) * p.q_row + (int64_t)head * p.q_head, here, p.dim, lane);
+  w.limit = here ? (int)query + off : -1;
+  w.clear();
+  const int low = (int)divide(block * 32u, p.by_rep) + off;  // last key of the wave's first query
+
+  const _Float16* K = p.K + s.k0 * p.k_row + (int64_t)g * p.k_head;
+  const _Float16* V = p.V + s.k0 * p.v_row + (int64_t)g * p.v_head;
+  auto issue = [&](uint32_t key, uint32_t to) {
+    const uint32_t left = key < end ? end - key : 0u;
+    stage<DP, kFewKeys, 64>(K + (int64_t)key * p.k_row, p.k_row, left, p.dim, to, lane);
+    stage<DP, kFewKeys, 64>(V + (int64_t)key * p.v_row, p.v_row, left, p.dim, to + kBytes, lane);
+  };
+  constexpr uint32_t kStep = kFewWaves * kFewKeys;
+  auto tile = [&](uint32_t key, const uint8_t* at, uint32_t lds) {
+    // all but the other stage's loads, which were issued after this one's
+    if (DP == 128) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+    if (key < end) {
+      if ((int)(key + kFewKeys) - 1 <= low) attend<DP, 1, false>(w, at, at + kBytes, (int)key, p.scale_log2, lane);
+      else attend<DP, 1, true>(w, at, at + kBytes, (int)key, p.scale_log2, lane);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile has been read
+    issue(key + 2u * kStep, lds);
+  };
+  uint32_t key = begin + wave * kFewKeys;
+  const uint32_t lds0 = lds_at(stage0[wave]), lds1 = lds_at(stage1[wave]);
+  __builtin_amdgcn_s_waitcnt(0);  // the queries have come: the compiler has nothing to wait for among the loop's loads
+  issue(key, lds0);
+  issue(key + kStep, lds1);
+  for (; key < end; key += 2u * kStep) {
+    tile(key, stage0[wave], lds0);
+    tile(key + kStep, stage1[wave], lds1);
+  }
+  __builtin_amdgcn_s_waitcnt(0);  // no load into LDS is left
+  __syncthreads();
+
+  // the waves' sums, brought to the largest of their m
+  w.l = across(w.l, true);
+  if (lane < 32u) top[wave][lane] = w.m;
+  __syncthreads();
+  float m = top[0][lane & 31u];
+#pragma unroll
+  for (uint32_t i = 1; i < kFewWaves; ++i) m = fmaxf(m, top[i][lane & 31u]);
+  const float down = w.m == -kInf ? 0.f : __builtin_amdgcn_exp2f(w.m - m);
+  if (lane < 32u) sum[wave][lane] = w.l * down;
+  // [wave][d / 4][query][4], in the stages' place
+  float* all = (float*)stage0;
+  static_assert(sizeof(stage0) >= sizeof(float) * (kFewWaves - 1) * 32 * DP, "fits");
+  if (wave != 0u) {
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const uint32_t quad = d * 8u + a * 2u + (lane >> 5);
+        *(float4v*)(all + (((wave - 1u) * (DP / 4) + quad) * 32u + (lane & 31u)) * 4u) =
+            float4v{w.o[d][4 * a] * down, w.o[d][4 * a + 1] * down, w.o[d][4 * a + 2] * down, w.o[d][4 * a + 3] * down};
+      }
+  }
+  __syncthreads();
+  if (wave != 0u || !here) return;
+  float l = sum[0][lane & 31u];
+#pragma unroll
+  for (uint32_t i = 1; i < kFewWaves; ++i) l += sum[i][lane & 31u];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      const uint32_t quad = d * 8u + a * 2u + (lane >> 5);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w.o[d][4 * a + e] *= down;
+#pragma unroll
+      for (uint32_t i = 1; i < kFewWaves; ++i) {
+        const float4v other = *(const float4v*)(all + (((i - 1u) * (DP / 4) + quad) * 32u + (lane & 31u)) * 4u);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w.o[d][4 * a + e] += other[e];
+      }
+    }
+  const int64_t row = s.q0 + query;
+  if (p.chunks == 1u) {
+    store_rows<DP>(w, p.O + row * p.o_row + (int64_t)head * p.o_head, l > 0.f ? 1.f / l : l, p.dim, lane);
+    if (p.lse && lane < 32u) p.lse[(int64_t)head * p.q_rows + row] = log_sum(m, l);
+    return;
+  }
+  const uint64_t at = ((uint64_t)c * p.part_rows + (uint64_t)b * p.max_q + query) * p.heads + head;
+  float* out = p.part_o + at * DP;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+      *(float4v*)(out + d * 32 + a * 8 + (lane >> 5) * 4u) = float4v{w.o[d][4 * a], w.o[d][4 * a + 1], w.o[d][4 * a + 2], w.o[d][4 * a + 3]};
+  if (lane < 32u) {
+    p.part_ml[at * 2] = m;
+    p.part_ml[at * 2 + 1] = l;
+  }
+}
+
+// --- chunks joined --------------------------------------------------------------------------------------------------------------
+// A block has a query row and 256 / (DP / 4) heads; four d to a lane.  Chunks are added in their order.
+template <int DP>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p) {
+  const uint32_t lane = threadIdx.x & 63u;
+  const int64_t row = blockIdx.x;
+  uint32_t b = 0;
+  for (uint32_t at = 0; at < p.sequences; at += 64u) {
+    const uint32_t i = at + lane;
+    b += __popcll(__ballot(i < p.sequences && p.q_start[i] <= row));
+  }
+  const uint32_t head = blockIdx.y * (1024u / DP) + threadIdx.x / (DP / 4), d = threadIdx.x % (DP / 4) * 4u;
+  if (b == 0u || head >= p.heads) return;
+  const Sequence s = sequence(p, b - 1u);
+  if (row < s.q0 || row >= s.q0 + s.nq) return;
+  const uint32_t n = min((s.nk + p.chunk - 1u) / p.chunk, p.chunks);
+  const uint64_t part_row = p.few ? (uint64_t)(b - 1u) * p.max_q + (uint64_t)(row - s.q0) : (uint64_t)row;
+  float m = -kInf, l = 0.f;
+  float4v o = {0.f, 0.f, 0.f, 0.f};
+  for (uint32_t c = 0; c < n; ++c) {
+    const uint64_t at = ((uint64_t)c * p.part_rows + part_row) * p.heads + head;
+    const float mc = p.part_ml[at * 2], lc = p.part_ml[at * 2 + 1];
+    const float4v oc = *(const float4v*)(p.part_o + at * DP + d);
+    if (mc == -kInf && lc == 0.f) continue;  // the query sees no key of the chunk
+    const float top = fmaxf(m, mc), old = m == -kInf ? 0.f : __builtin_amdgcn_exp2f(m - top), now = __builtin_amdgcn_exp2f(mc - top);
+    l = l * old + lc * now;
+    o = o * old + oc * now;
+    m = top;
+  }
+  if (d == 0u && p.lse) p.lse[(int64_t)head * p.q_rows + row] = log_sum(m, l);
+  if (d >= p.dim) return;
+  const float factor = l > 0.f ? 1.f / l : l;
+  *(half4*)(p.O + row * p.o_row + (int64_t)head * p.o_head + d) =
+      half4{(_Float16)(o[0] * factor), (_Float16)(o[1] * factor), (_Float16)(o[2] * factor), (_Float16)(o[3] * factor)};
+}
+
+// --- host -----------------------------------------------------------------------------------------------------------------------
+
+static uint32_t padded_dim(uint32_t dim) { return dim <= 64 ? 64 : 128; }
+
+AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads, uint32_t kv_heads, uint32_t dim, int64_t max_q, int64_t max_k) {
+  AttentionPlan plan = {};
+  const uint64_t packed = (uint64_t)max_q * (heads / kv_heads);  // rows of queries that share keys
+  plan.few = packed <= 64 ? 1u : 0u;
+  plan.row_blocks = (uint32_t)((packed + 31) / 32);
+  // workgroups with work if the keys are not split: about
+  const uint64_t busy = plan.few ? (uint64_t)sequences * kv_heads * plan.row_blocks : ((uint64_t)q_rows + kTileQ - 1) / kTileQ * heads;
+  const uint64_t wanted = (plan.few ? 1024u : 512u) / (busy ? busy : 1), most = ((uint64_t)max_k + 255) / 256;
+  uint64_t chunks = wanted < most ? wanted : most;
+  if (chunks < 1) chunks = 1;
+  plan.chunk = (uint32_t)((((uint64_t)max_k + chunks - 1) / chunks + 127) / 128 * 128);
+  if (plan.chunk == 0) plan.chunk = 128;
+  plan.chunks = (uint32_t)(((uint64_t)max_k + plan.chunk - 1) / plan.chunk);
+  if (plan.chunks == 0) plan.chunks = 1;
+  plan.part_rows = plan.few ? (uint64_t)sequences * max_q : (uint64_t)q_rows;
+  plan.parts_bytes = plan.chunks > 1 ? plan.part_rows * heads * plan.chunks * (padded_dim(dim) + 2) * sizeof(float) : 0;
+  plan.slots = (uint32_t)(q_rows / kTileQ) + sequences;
+  plan.units = (plan.few ? busy : (uint64_t)plan.slots * heads) * plan.chunks;
+  return plan;
+}
+
+template <int DP>
+static hipError_t run(AttentionParams& p, const AttentionPlan& plan, hipStream_t stream) {
+  if (plan.few) attention_few_kernel<DP><<<p.units, kFewWaves * 64, 0, stream>>>(p);
+  else attention_kernel<DP><<<(p.units + 7u) / 8u * 8u, 256, 0, stream>>>(p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.chunks == 1u) return e;
+  attention_join_kernel<DP><<<dim3((uint32_t)p.q_rows, (p.heads + 1024 / DP - 1) / (1024 / DP)), 256, 0, stream>>>(p);
+  return hipGetLastError();
+}
+
+hipError_t launch_attention(const AttentionLaunch& a, const AttentionPlan& plan, hipStream_t stream) {
+  const uint32_t DP = padded_dim(a.dim);
+  AttentionParams p = {};
+  p.Q = a.Q, p.K = a.K, p.V = a.V, p.O = a.O, p.lse = a.lse;
+  p.q_start = a.q_start, p.k_start = a.k_start, p.k_len = a.k_len;
+  p.q_rows = a.q_rows, p.k_rows = a.k_rows;
+  p.q_row = a.q_row, p.q_head = a.q_head, p.k_row = a.k_row, p.k_head = a.k_head, p.v_row = a.v_row, p.v_head = a.v_head, p.o_row = a.o_row, p.o_head = a.o_head;
+  p.sequences = a.sequences, p.heads = a.heads, p.rep = a.heads / a.kv_heads, p.dim = a.dim, p.max_q = (uint32_t)a.max_q, p.max_k = (uint32_t)a.max_k;
+  p.chunk = plan.chunk, p.chunks = plan.chunks;
+  p.scale_log2 = a.scale * 1.44269504088896341f;
+  p.part_o = a.parts;
+  p.part_ml = a.parts + plan.chunks * plan.part_rows * a.heads * DP;
+  p.part_rows = plan.part_rows;
+  p.few = plan.few;
+  p.by_rep = divisor(p.rep), p.by_chunks = divisor(p.chunks), p.by_kv_heads = divisor(a.kv_heads);
+  p.row_blocks = plan.row_blocks, p.slots = plan.slots, p.units = (uint32_t)plan.units;
+  p.by_row_blocks = divisor(plan.few ? p.row_blocks : 1u), p.by_slots = divisor(p.slots);
+  return DP == 64 ? run<64>(p, plan, stream) : run<128>(p, plan, stream);
+}
+
+}  // namespace fls

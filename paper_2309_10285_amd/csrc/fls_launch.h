@@ -430,21 +430,24 @@ struct AttentionLaunch {
   float* lse;  // [heads][q_rows] or null
   const int32_t *q_start, *k_start, *k_len;
   int64_t q_rows, k_rows, q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
-  uint32_t sequences, heads, kv_heads, dim, max_q;
-  int64_t max_k;
+  uint32_t sequences, heads, kv_heads, dim;
+  int64_t max_q, max_k;
   float scale;
   float* parts;
-  int num_cus;
 };
 // How a call is cut.
 struct AttentionPlan {
   uint32_t few;        // 1: the kernel for few queries to a sequence
   uint32_t chunk;      // keys to a workgroup, a multiple of 128; all of them where `chunks` is 1
   uint32_t chunks;     // at most that many chunks to a sequence
+  uint32_t row_blocks; // of 32 rows of queries, where there are few
+  uint32_t slots;      // of 128 queries
+  uint64_t part_rows;  // rows of sums to a chunk, each with all heads
   size_t parts_bytes;
+  uint64_t units;      // workgroups, also those with no work
 };
-AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t max_q, int64_t max_k);
-hipError_t launch_attention(const AttentionLaunch& a, hipStream_t stream);
+AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads, uint32_t kv_heads, uint32_t dim, int64_t max_q, int64_t max_k);
+hipError_t launch_attention(const AttentionLaunch& a, const AttentionPlan& plan, hipStream_t stream);
 
 }  // namespace fls
 
