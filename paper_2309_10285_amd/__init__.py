@@ -109,6 +109,8 @@ def lib():
         L.fls_attention_workspace_bytes.restype = sz
         L.fls_attention.argtypes = [vp] * 10
         L.fls_attention.restype = ci
+        L.fls_internal_fp8_plan.argtypes = [ctypes.c_uint32] * 3 + [ci, ctypes.POINTER(ctypes.c_uint32)]
+        L.fls_internal_fp8_plan.restype = None
         L.fls_internal_spmm_plan.argtypes = [ctypes.c_uint32] * 5 + [ci, ci, ctypes.POINTER(ctypes.c_uint32)]
         L.fls_internal_spmm_plan.restype = None
         L.fls_strerror.argtypes = [ci]

@@ -564,7 +564,7 @@ static bool fp8_layout(int64_t M, int64_t K, int64_t N, size_t* xq, size_t* xs, 
   if (!fp8_shape_ok(M, K) || N < 1 || N > FLS_MAX_N) return false;
   if ((uint64_t)K * (uint64_t)N * 2u > 0x7fffffffull || (uint64_t)M * (uint64_t)N * 2u > 0x7fffffffull) return false;
   *xq = kCounterAreaBytes + fls::fp8_parts_bytes();
-  *xs = *xq + round_up((uint64_t)N * (uint64_t)K, 16);
+  *xs = *xq + fls::fp8_xq_bytes((uint32_t)K, (uint32_t)N);
   *total = *xs + round_up((uint64_t)N * fls::scale_stride((uint32_t)K), 16);
   return true;
 }
@@ -685,6 +685,14 @@ void fls_internal_spmm_plan(uint32_t max_tile_words, uint32_t version, uint32_t 
 void fls_internal_dense_plan(uint32_t M, uint32_t K, uint32_t N, int cus, uint32_t* out) {
   out[0] = fls::dense_col_groups(M, K, N, cus);
   out[1] = fls::wide_slices(M / FLS_TILE_M, out[0], (K + 63u) / 64u, cus);
+}
+
+void fls_internal_fp8_plan(uint32_t M, uint32_t K, uint32_t N, int cus, uint32_t* out) {
+  const fls::Fp8Plan plan = fls::fp8_plan(M, K, N, cus);
+  out[0] = (uint32_t)plan.pass;
+  out[1] = plan.tile_m;
+  out[2] = plan.tile_n;
+  out[3] = plan.slices;
 }
 
 void fls_internal_shares(uint32_t M, uint32_t K, int cus, float tile_us, int wide, uint32_t* out) {

@@ -63,31 +63,19 @@ __device__ __forceinline__ uint32_t turn(uint32_t row) {
   return DP == 128 ? ((row & 7u) << 1 | (row >> 3 & 1u)) : ((row & 3u) << 1 | (row >> 2 & 1u));
 }
 
-// Where an array lies in LDS.
-__device__ __forceinline__ uint32_t lds_at(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
-
-// 16 bytes to a lane straight to LDS at `lds` + 16 lane (`lds` the same for the wave).  An asm statement, because the compiler waits for all loads into LDS
-// before it reads LDS with a transposing read, which would leave nothing in flight.  It writes no register but m0, which nothing else in these kernels
-// uses (the compiler keeps nothing there); who reads the LDS waits for it (vmcnt).
-__device__ __forceinline__ void load_lds(u32x4 buf, uint32_t lds, uint32_t off) {
-  const uint32_t at = __builtin_amdgcn_readfirstlane(lds);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(buf) : "memory");
-}
-
 // ROWS rows of DP values to LDS by THREADS lanes; rows from `left` on and values from dim on are 0.
 template <int DP, int ROWS, int THREADS>
 __device__ __forceinline__ void stage(const _Float16* first, int64_t row_stride, uint32_t left, uint32_t dim, uint32_t lds, uint32_t thread) {
   constexpr uint32_t kPieces = DP / 8, kStep = THREADS / kPieces;  // rows to a load of all lanes
   static_assert(ROWS % kStep == 0 && (kStep % 16 == 0 || 16 % kStep == 0), "whole loads");
   const uint32_t bytes = left == 0u ? 0u : (uint32_t)((min(left, (uint32_t)ROWS) - 1u) * row_stride * 2 + dim * 2u);
-  const uint64_t base = (uint64_t)first;
-  const u32x4 buf = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, bytes, (uint32_t)kBufferFlags};  // raw buffer of `bytes` from `first` on
+  const u32x4 buf = descriptor(first, bytes);
   const uint32_t wave = __builtin_amdgcn_readfirstlane(thread >> 6);
 #pragma unroll
   for (int i = 0; i < ROWS / (int)kStep; ++i) {
     const uint32_t row = i * kStep + thread / kPieces, piece = (thread % kPieces) ^ turn<DP>(row);
     const uint32_t off = row * (uint32_t)(row_stride * 2) + piece * 16u;
-    load_lds(buf, lds + i * THREADS * 16 + wave * 1024u, row < left && piece * 8u < dim ? off : kNowhere);
+    load_lds<16>(buf, lds + i * THREADS * 16 + wave * 1024u, row < left && piece * 8u < dim ? off : kNowhere);
   }
 }
 

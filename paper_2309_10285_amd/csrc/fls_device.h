@@ -36,6 +36,27 @@ __device__ __forceinline__ uint32_t scatter_addr(uint32_t word, uint32_t base) {
   return addr;
 }
 
+// Where an array lies in LDS.
+__device__ __forceinline__ uint32_t lds_at(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
+
+// A raw buffer of `bytes` (up to 2^31) from p on, as the asm statement below takes it: offsets from `bytes` on give 0.
+__device__ __forceinline__ u32x4 descriptor(const void* p, uint64_t bytes) {
+  const uint64_t base = (uint64_t)p;
+  return u32x4{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, (uint32_t)(bytes < 0x7fffffffull ? bytes : 0x7fffffffull), (uint32_t)kBufferFlags};
+}
+
+// 16 (or 4) bytes to a lane straight to LDS at `lds` + 16 (4) lane (`lds` the same for the wave).  An asm statement, because the compiler waits for
+// loads into LDS that it knows of wherever it cannot tell what is read (a ring of stages, a transposing read), and at barriers, which would leave
+// nothing in flight.  It writes no register but m0, which nothing else in the kernels that use it needs (the compiler keeps nothing there);
+// who reads the LDS waits for it (vmcnt).
+template <int BYTES>
+__device__ __forceinline__ void load_lds(u32x4 buf, uint32_t lds, uint32_t off) {
+  static_assert(BYTES == 16 || BYTES == 4, "");
+  const uint32_t at = __builtin_amdgcn_readfirstlane(lds);
+  if (BYTES == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(buf) : "memory");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(buf) : "memory");
+}
+
 // What both kernels need to hand results over.
 //
 // Split-K: the band-major tile sequence [0, T) is cut evenly over the workgroups, then over the

@@ -403,10 +403,17 @@ inline uint32_t scale_stride(uint32_t K) { return (K + 511u) / 512u * 4u; }
 // Room for the sums of K slices.
 constexpr size_t fp8_parts_bytes() { return (size_t)64 << 20; }
 
+// Groups of 16 columns of the kernel that streams W (up to 64 columns), and bytes for X quantised: for that kernel whole steps in fragment order.
+inline uint32_t fp8_column_groups(uint32_t N) { return N <= 16 ? 1 : N <= 32 ? 2 : 4; }
+inline size_t fp8_xq_bytes(uint32_t K, uint32_t N) {
+  return N <= 64 ? (size_t)((K + 127) / 128) * fp8_column_groups(N) * 2048 : ((size_t)N * K + 15) / 16 * 16;
+}
+
 enum { kFp8StreamQuant, kFp8Stream, kFp8Tile };
 struct Fp8Plan {
   int pass;
-  uint32_t slices;
+  uint32_t tile_m, tile_n;  // of a workgroup, tile_n for kFp8Tile only
+  uint32_t slices;          // of K
 };
 Fp8Plan fp8_plan(uint32_t M, uint32_t K, uint32_t N, int cus);
 
@@ -415,7 +422,7 @@ struct Fp8Launch {
   const _Float16* X;
   _Float16* C;
   float* parts;       // fp8_parts_bytes()
-  uint8_t *Xq, *Xs;   // N x K and N x scale_stride(K) bytes, for X quantised
+  uint8_t *Xq, *Xs;   // fp8_xq_bytes(K, N) and N x scale_stride(K) bytes, for X quantised
   uint32_t M, K, N;
   int num_cus;
 };
@@ -459,6 +466,9 @@ extern "C" void fls_internal_spmm_plan(uint32_t max_tile_words, uint32_t version
 
 // What fls_dense_gemm of more than 32 columns launches first: out = groups of 64 columns, K slices.  As above.
 extern "C" void fls_internal_dense_plan(uint32_t M, uint32_t K, uint32_t N, int cus, uint32_t* out);
+
+// What fls_fp8_gemm runs: out = pass (0: streamed, X quantised on the way, 1: streamed, 2: tiles), tile_m, tile_n, slices of Fp8Plan.  As above.
+extern "C" void fls_internal_fp8_plan(uint32_t M, uint32_t K, uint32_t N, int cus, uint32_t* out);
 
 // How the tiles of an M x K matrix are shared out in the passes of up to 32 columns: out = P, unit, grid of Shares.  As above.
 extern "C" uint32_t fls_internal_divide(uint32_t n, uint32_t d);  // as the kernels divide

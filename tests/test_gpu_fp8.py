@@ -118,7 +118,8 @@ def run(fls, W, X, fill=7.0):
 SHAPES = [(1, 16, 1), (16, 128, 1), (17, 144, 16), (5, 400, 3), (64, 1040, 15), (1000, 528, 7), (257, 2048, 13), (1024, 1024, 1),
           (130, 640, 17), (63, 1024, 32), (300, 400, 33), (129, 4096, 64), (64, 9216, 50),
           (1, 16, 65), (256, 128, 256), (255, 272, 100), (257, 384, 257), (1000, 1152, 300), (513, 4096, 129), (40, 16384, 70), (3000, 640, 700),
-          (777, 1040, 1111), (4097, 512, 2049), (2048, 8192, 16), (128, 32768, 8), (128, 32768, 40), (100, 32768, 90)]
+          (777, 1040, 1111), (4097, 512, 2049), (2048, 8192, 16), (128, 32768, 8), (128, 32768, 40), (100, 32768, 90),
+          (128, 33040, 5), (70, 65552, 60), (300, 2304, 200), (260, 7184, 130), (5000, 2560, 20), (9000, 2064, 300), (33000, 272, 14), (2000, 9216, 1), (1100, 5136, 1000)]
 
 
 @pytest.mark.parametrize("M,K,N", SHAPES)
