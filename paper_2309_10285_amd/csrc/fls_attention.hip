@@ -2,9 +2,11 @@
 //
 //   s_ij = scale q_i . k_j for j <= i + keys - queries,   o_i = sum_j exp(s_ij) v_j / sum_j exp(s_ij)
 //
-// A query keeps the largest score so far m (times log2 e: powers of two are what the hardware computes), the sum l of 2^(s - m) and
-// the sum o of 2^(s - m) v; when m grows, l and o are multiplied by 2^(old - new).  All three are fp32; 2^(s - m) is rounded to fp16
-// for the product with v (to nearest, 2^-11 of it), raised by 2^kLift so that what is small beside the largest is not subnormal.
+// A query keeps a score m (times log2 e: powers of two are what the hardware computes), the sum l of 2^(s - m) and the sum o of
+// 2^(s - m) v.  When a score exceeds m by more than kSlack, m becomes the largest score so far and l and o are multiplied by 2^(old - new); to
+// do that for every new largest score would cost as much as a fifth of the other vector work.  All three are fp32; 2^(s - m) is rounded to
+// fp16 for the product with v (to nearest, 2^-11 of it), raised by 2^kLift so that what is small beside the largest is not subnormal:
+// at most 2^(kLift + kSlack), half of what fp16 holds.
 //
 // Both products are computed transposed, with 32x32x16 MFMAs: S^T = K Q^T gives lane l the column of query l & 31 and of 32 keys the rows
 // 8 a + 4 (l >> 5) + b (a, b = 0 ... 3), so that the largest and the sum of a query's scores are found inside a lane and
@@ -21,7 +23,7 @@ namespace fls {
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 
-constexpr int kLift = 12;
+constexpr int kLift = 7, kSlack = 8;
 constexpr uint32_t kNowhere = 0x80000000u;  // an offset past every buffer descriptor here: a load from it gives 0
 constexpr float kInf = __builtin_inff();
 
@@ -58,15 +60,21 @@ __device__ __forceinline__ Sequence sequence(const AttentionParams& p, uint32_t 
   return s;
 }
 
+// Head sizes are filled up to DP = 64, 96 or 128 with zeros; a row in LDS has 64 or 128 values.
+template <int DP>
+constexpr int kPitch = DP == 64 ? 64 : 128;
+
+// Where a row's pieces lie.  128 values: 16 rows give a piece 16 places (256 B, all banks), four neighbouring rows four pieces 16 places.
+// 64 values: the same of eight and four pairs of rows.
 template <int DP>
 __device__ __forceinline__ uint32_t turn(uint32_t row) {
-  return DP == 128 ? ((row & 7u) << 1 | (row >> 3 & 1u)) : ((row & 3u) << 1 | (row >> 2 & 1u));
+  return DP == 64 ? (row >> 1 & 1u) << 2 | (row >> 2 & 3u) : (row & 3u) << 2 | (row >> 2 & 3u);
 }
 
-// ROWS rows of DP values to LDS by THREADS lanes; rows from `left` on and values from dim on are 0.
+// ROWS rows to LDS by THREADS lanes; rows from `left` on and values from dim on are 0.
 template <int DP, int ROWS, int THREADS>
 __device__ __forceinline__ void stage(const _Float16* first, int64_t row_stride, uint32_t left, uint32_t dim, uint32_t lds, uint32_t thread) {
-  constexpr uint32_t kPieces = DP / 8, kStep = THREADS / kPieces;  // rows to a load of all lanes
+  constexpr uint32_t kPieces = kPitch<DP> / 8, kStep = THREADS / kPieces;  // rows to a load of all lanes
   static_assert(ROWS % kStep == 0 && (kStep % 16 == 0 || 16 % kStep == 0), "whole loads");
   const uint32_t bytes = left == 0u ? 0u : (uint32_t)((min(left, (uint32_t)ROWS) - 1u) * row_stride * 2 + dim * 2u);
   const u32x4 buf = descriptor(first, bytes);
@@ -116,7 +124,7 @@ __device__ __forceinline__ float across(float x, bool add) {  // with the lane 3
 template <int DP>
 __device__ __forceinline__ float16v scores(const Wave<DP>& w, const uint8_t* tile, uint32_t lane) {
   float16v s = {};
-  const uint8_t* row = tile + (lane & 31u) * (DP * 2);
+  const uint8_t* row = tile + (lane & 31u) * (kPitch<DP> * 2);
   const uint32_t t = turn<DP>(lane & 31u) ^ (lane >> 5);
 #pragma unroll
   for (int i = 0; i < DP / 16; ++i) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)(row + ((2u * i ^ t) << 4)), w.q[i], s, 0, 0, 0);
@@ -128,26 +136,37 @@ template <int DP>
 __device__ __forceinline__ half8 values(const uint8_t* tile, uint32_t key, uint32_t d, uint32_t lane) {
   const uint32_t row = key + 4u * (lane >> 5) + ((lane & 15u) >> 2), piece = d / 8u + 2u * ((lane >> 4) & 1u) + ((lane & 3u) >> 1);
   typedef __attribute__((address_space(3))) short4v* lds_ptr;
-  const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + row * (DP * 2) + ((piece ^ turn<DP>(row)) << 4) + (lane & 1u) * 8u));
-  const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + (row + 8u) * (DP * 2) + ((piece ^ turn<DP>(row + 8u)) << 4) + (lane & 1u) * 8u));
+  const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + row * (kPitch<DP> * 2) + ((piece ^ turn<DP>(row)) << 4) + (lane & 1u) * 8u));
+  const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + (row + 8u) * (kPitch<DP> * 2) + ((piece ^ turn<DP>(row + 8u)) << 4) + (lane & 1u) * 8u));
   return __builtin_bit_cast(half8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 // Key of score i of a lane.
 __device__ __forceinline__ uint32_t key_of(int i, uint32_t lane) { return 8u * (i / 4) + 4u * (lane >> 5) + i % 4; }
 
-// Weights of 32 B keys from their scores: m, l and o are brought up to date, s becomes 2^(s - m + kLift).
+// Makes m fit 32 B keys with these scores.
 template <int DP, int B>
-__device__ __forceinline__ void soften(Wave<DP>& w, float16v (&s)[B], float scale_log2) {
+__device__ __forceinline__ void settle(Wave<DP>& w, const float16v (&s)[B], float scale_log2) {
   float top = s[0][0];
 #pragma unroll
   for (int b = 0; b < B; ++b)
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-  const float m = fmaxf(w.m, across(top, false) * scale_log2);
-  const float base = m == -kInf ? 0.f : m - kLift;  // a query that has seen no key: its weights are 0, not NaN
-  const float down = __builtin_amdgcn_exp2f(w.m - (base + kLift));
+  top = across(top, false) * scale_log2;
+  if (!__any(top > w.m + kSlack)) return;
+  const float m = fmaxf(w.m, top), down = m == -kInf ? 0.f : __builtin_amdgcn_exp2f(w.m - m);
   w.m = m;
+  w.l *= down;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w.o[d][i] *= down;
+}
+
+// Their weights in their place, added to l.
+template <int DP, int B>
+__device__ __forceinline__ void soften(Wave<DP>& w, float16v (&s)[B], float scale_log2) {
+  const float base = w.m == -kInf ? 0.f : w.m - kLift;  // a query that has seen no key: its weights are 0, not NaN
   float sum = 0.f;
 #pragma unroll
   for (int b = 0; b < B; ++b)
@@ -156,11 +175,7 @@ __device__ __forceinline__ void soften(Wave<DP>& w, float16v (&s)[B], float scal
       s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], scale_log2, -base));
       sum += s[b][i];
     }
-  w.l = w.l * down + sum;  // of this lane's keys; both lanes' in the end
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) w.o[d][i] *= down;
+  w.l += sum;  // of this lane's keys; both lanes' in the end
 }
 
 __device__ __forceinline__ half8 weights(const float16v& s, int half) {
@@ -185,7 +200,7 @@ template <int DP, int ROWS>
 __device__ __forceinline__ bool any_not_finite(const uint8_t* tile, uint32_t lane) {
   bool found = false;
 #pragma unroll
-  for (int i = 0; i < ROWS * DP / 512; ++i) {
+  for (int i = 0; i < ROWS * kPitch<DP> / 512; ++i) {
     const half8 v = *(const half8*)(tile + (i * 64u + lane) * 16u);
 #pragma unroll
     for (int e = 0; e < 8; ++e) found |= !(__builtin_fabsf16(v[e]) <= (_Float16)65504.f);
@@ -227,13 +242,14 @@ __device__ __forceinline__ void attend(Wave<DP>& w, const uint8_t* k_tile, const
   float16v s[B];
 #pragma unroll
   for (int b = 0; b < B; ++b) {
-    s[b] = scores<DP>(w, k_tile + b * 32 * DP * 2, lane);
+    s[b] = scores<DP>(w, k_tile + b * 32 * kPitch<DP> * 2, lane);
     if (MASK) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (key0 + (int)(b * 32u + key_of(i, lane)) > w.limit) s[b][i] = -kInf;
     }
   }
+  settle<DP, B>(w, s, scale_log2);
   soften<DP, B>(w, s, scale_log2);
   if (MASK && any_not_finite<DP, 32 * B>(v_tile, lane)) add_seen_values<DP, B>(w, s, v_tile, key0, lane);
   else add_values<DP, B>(w, s, v_tile, lane);
@@ -263,7 +279,7 @@ constexpr uint32_t kTileQ = 128, kTileKeys = 64;
 
 template <int DP>
 __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
-  constexpr int kBytes = kTileKeys * DP * 2;
+  constexpr int kBytes = kTileKeys * kPitch<DP> * 2;
   __shared__ __align__(16) uint8_t stages[2][2 * kBytes];  // a tile of K, one of V
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t unit;
@@ -328,7 +344,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
 #pragma unroll 1
     for (uint32_t half = 0; half < 2u; ++half) {  // half a tile at a time: with a mask, a whole one needs more registers than there are
       const int key0 = (int)(t * kTileKeys + half * 32u);
-      if (key0 <= high) attend<DP, 1, true>(w, stages[now] + half * 32u * DP * 2, stages[now] + kBytes + half * 32u * DP * 2, key0, p.scale_log2, lane);
+      if (key0 <= high) attend<DP, 1, true>(w, stages[now] + half * (kBytes / 2), stages[now] + kBytes + half * (kBytes / 2), key0, p.scale_log2, lane);
     }
   }
   w.l = across(w.l, true);
@@ -361,7 +377,7 @@ constexpr uint32_t kFewWaves = 2, kFewKeys = 32;
 
 template <int DP>
 __global__ __launch_bounds__(kFewWaves * 64) void attention_few_kernel(AttentionParams p) {
-  constexpr int kBytes = kFewKeys * DP * 2;
+  constexpr int kBytes = kFewKeys * kPitch<DP> * 2;
   __shared__ __align__(16) uint8_t stage0[kFewWaves][2 * kBytes], stage1[kFewWaves][2 * kBytes];
   __shared__ float top[kFewWaves][32], sum[kFewWaves][32];
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -397,7 +413,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_few_kernel(Attention
   constexpr uint32_t kStep = kFewWaves * kFewKeys;
   auto tile = [&](uint32_t key, const uint8_t* at, uint32_t lds) {
     // all but the other stage's loads, which were issued after this one's
-    if (DP == 128) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+    if (kPitch<DP> == 128) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
     else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
     if (key < end) {
       if ((int)(key + kFewKeys) - 1 <= low) attend<DP, 1, false>(w, at, at + kBytes, (int)key, p.scale_log2, lane);
@@ -479,7 +495,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_few_kernel(Attention
 }
 
 // --- chunks joined --------------------------------------------------------------------------------------------------------------
-// A block has a query row and 256 / (DP / 4) heads; four d to a lane.  Chunks are added in their order.
+// A block has a query row and 8 or 16 heads; four d to a lane.  Chunks are added in their order.
 template <int DP>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p) {
   const uint32_t lane = threadIdx.x & 63u;
@@ -489,8 +505,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p) 
     const uint32_t i = at + lane;
     b += __popcll(__ballot(i < p.sequences && p.q_start[i] <= row));
   }
-  const uint32_t head = blockIdx.y * (1024u / DP) + threadIdx.x / (DP / 4), d = threadIdx.x % (DP / 4) * 4u;
-  if (b == 0u || head >= p.heads) return;
+  const uint32_t head = blockIdx.y * (1024u / kPitch<DP>) + threadIdx.x / (kPitch<DP> / 4), d = threadIdx.x % (kPitch<DP> / 4) * 4u;
+  if (b == 0u || head >= p.heads || d >= (uint32_t)DP) return;
   const Sequence s = sequence(p, b - 1u);
   if (row < s.q0 || row >= s.q0 + s.nq) return;
   const uint32_t n = min((s.nk + p.chunk - 1u) / p.chunk, p.chunks);
@@ -516,7 +532,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p) 
 
 // --- host -----------------------------------------------------------------------------------------------------------------------
 
-static uint32_t padded_dim(uint32_t dim) { return dim <= 64 ? 64 : 128; }
+static uint32_t padded_dim(uint32_t dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : 128; }
 
 AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads, uint32_t kv_heads, uint32_t dim, int64_t max_q, int64_t max_k) {
   AttentionPlan plan = {};
@@ -545,7 +561,7 @@ static hipError_t run(AttentionParams& p, const AttentionPlan& plan, hipStream_t
   else attention_kernel<DP><<<(p.units + 7u) / 8u * 8u, 256, 0, stream>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.chunks == 1u) return e;
-  attention_join_kernel<DP><<<dim3((uint32_t)p.q_rows, (p.heads + 1024 / DP - 1) / (1024 / DP)), 256, 0, stream>>>(p);
+  attention_join_kernel<DP><<<dim3((uint32_t)p.q_rows, (p.heads + 1024 / kPitch<DP> - 1) / (1024 / kPitch<DP>)), 256, 0, stream>>>(p);
   return hipGetLastError();
 }
 
@@ -566,7 +582,7 @@ hipError_t launch_attention(const AttentionLaunch& a, const AttentionPlan& plan,
   p.by_rep = divisor(p.rep), p.by_chunks = divisor(p.chunks), p.by_kv_heads = divisor(a.kv_heads);
   p.row_blocks = plan.row_blocks, p.slots = plan.slots, p.units = (uint32_t)plan.units;
   p.by_row_blocks = divisor(plan.few ? p.row_blocks : 1u), p.by_slots = divisor(p.slots);
-  return DP == 64 ? run<64>(p, plan, stream) : run<128>(p, plan, stream);
+  return DP == 64 ? run<64>(p, plan, stream) : DP == 96 ? run<96>(p, plan, stream) : run<128>(p, plan, stream);
 }
 
 }  // namespace fls

@@ -3,7 +3,8 @@
 Bounds, for a query with S = the largest scale |q| . |k| of its keys, n keys, and A = sum of weights times |v|:
   a score is a sum of head_dim products in fp32: off by at most (head_dim + 8) 2^-24 S, a few roundings of its own among them;
   a weight by as much again for the exponential's argument, and by 2^-21 for what the hardware's 2^x leaves;
-  weights are rounded to fp16 for the product with V: half a step, 2^-11 of a weight (those under 2^-26 of the largest: 2^-37);
+  weights are rounded to fp16 for the product with V: half a step, 2^-11 of a weight; they are powers 2^(s - m + 7) of an m that is at most the largest
+  score, so those under fp16's normal range, 2^-14, are off by at most 2^-25 / 2^7 of a weight at m, 2^-32 of the largest;
   sums over the keys in fp32: (n + 64) 2^-24;  O is rounded once: 2^-11 of it, 2^-25 below fp16's normal range.
 """
 import math
@@ -56,7 +57,7 @@ def reference(Q, K, V, q_start, k_start, k_len, scale):
             lse[h, q0:q1] = (top + total.log())[:, 0]
             score = (D + 8) * 2.0 ** -24 * size
             A = w @ v0.abs()
-            off[q0:q1, h] = 2.0 ** -11 * O[q0:q1, h].abs().nan_to_num(0, 0, 0) + (2.0 ** -11 + 2 * (2 * score + 2.0 ** -21 + (nk + 64) * 2.0 ** -24))[:, None] * A + 2.0 ** -25 + 2.0 ** -37 * v0.abs().sum(0) if nk else 0.0
+            off[q0:q1, h] = 2.0 ** -11 * O[q0:q1, h].abs().nan_to_num(0, 0, 0) + (2.0 ** -11 + 2 * (2 * score + 2.0 ** -21 + (nk + 64) * 2.0 ** -24))[:, None] * A + 2.0 ** -25 + 2.0 ** -32 * v0.abs().sum(0) if nk else 0.0
             lse_off[h, q0:q1] = 2 * score + 2.0 ** -21 + (nk + 64) * 2.0 ** -24 + 2.0 ** -22 * lse[h, q0:q1].abs().nan_to_num(0, 0, 0)
     return O, off, lse, lse_off
 
