@@ -628,7 +628,7 @@ static bool attention_shape_ok(const fls_attention_shape* s, fls::AttentionPlan*
   if (!row_of_heads && !head_of_rows) return false;
   const int64_t max_q = s->max_q < s->q_rows ? s->max_q : s->q_rows, max_k = s->max_k < s->k_rows ? s->max_k : s->k_rows;
   *plan = fls::attention_plan(s->q_rows, (uint32_t)s->sequences, (uint32_t)s->heads, (uint32_t)s->kv_heads, (uint32_t)s->head_dim, max_q, max_k);
-  return plan->units < (1ull << 29);
+  return plan->units < (1ull << 29) && (plan->chunks == 1 || plan->part_rows * s->heads < (1ull << 29));
 }
 
 size_t fls_attention_workspace_bytes(const fls_attention_shape* shape_host) {

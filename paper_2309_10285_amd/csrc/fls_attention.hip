@@ -41,7 +41,7 @@ struct AttentionParams {
   float* part_ml;             // [chunk][part row][head][2]
   uint64_t part_rows;
   uint32_t few;
-  Divisor by_rep, by_chunks, by_row_blocks, by_kv_heads, by_slots;
+  Divisor by_rep, by_chunks, by_row_blocks, by_kv_heads, by_slots, by_heads, by_max_q;
 };
 
 // A sequence, cut to the tensors it lies in: whatever the arrays hold, nothing outside is read or written.
@@ -120,24 +120,45 @@ __device__ __forceinline__ float across(float x, bool add) {  // with the lane 3
   return add ? a + b : fmaxf(a, b);
 }
 
-// S^T of 32 keys, whose rows of K begin at `tile`.
+// Where a lane begins to read in a tile of K or V, from its start on.  All its other places differ from that in bits that pieces lie in (and in whole rows), so
+// they are one exclusive or away: kept in registers, they would be more than there are.
 template <int DP>
-__device__ __forceinline__ float16v scores(const Wave<DP>& w, const uint8_t* tile, uint32_t lane) {
-  float16v s = {};
-  const uint8_t* row = tile + (lane & 31u) * (kPitch<DP> * 2);
-  const uint32_t t = turn<DP>(lane & 31u) ^ (lane >> 5);
-#pragma unroll
-  for (int i = 0; i < DP / 16; ++i) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)(row + ((2u * i ^ t) << 4)), w.q[i], s, 0, 0, 0);
-  return s;
+__device__ __forceinline__ uint32_t key_place(uint32_t lane) {
+  const uint32_t row = lane & 31u;
+  return row * (kPitch<DP> * 2) + ((turn<DP>(row) ^ (lane >> 5)) << 4);
+}
+template <int DP>
+__device__ __forceinline__ uint32_t value_place(uint32_t lane) {
+  const uint32_t row = 4u * (lane >> 5) + ((lane & 15u) >> 2), piece = 2u * ((lane >> 4) & 1u) + ((lane & 3u) >> 1);
+  return row * (kPitch<DP> * 2) + ((piece ^ turn<DP>(row)) << 4) + (lane & 1u) * 8u;
+}
+__device__ __forceinline__ uint32_t place_in(uint32_t tile, uint32_t place) {
+  uint32_t at = tile + place;
+  asm volatile("" : "+v"(at));  // not known before the loop
+  return at;
 }
 
-// Eight keys of V^T for 32 d: keys key + 4 (l >> 5) + 0 ... 3 and the same 8 further, as S^T has them.
+typedef const __attribute__((address_space(3))) half8* lds_half8;
+
+// S^T of 32 B keys; `at`: key_place in their rows of K.  Block by block in turn: a product that waits for the one before it waits longer than it takes.
+template <int DP, int B>
+__device__ __forceinline__ void scores(const Wave<DP>& w, uint32_t at, float16v (&s)[B]) {
+#pragma unroll
+  for (int b = 0; b < B; ++b) s[b] = float16v{};
+#pragma unroll
+  for (uint32_t i = 0; i < DP / 16; ++i)
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+      s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(lds_half8)(uintptr_t)((at ^ (i << 5)) + b * (32 * kPitch<DP> * 2)), w.q[i], s[b], 0, 0, 0);
+}
+
+// Eight keys of V^T for 32 d: keys key + 4 (l >> 5) + 0 ... 3 and the same 8 further, as S^T has them; `at`: value_place.
 template <int DP>
-__device__ __forceinline__ half8 values(const uint8_t* tile, uint32_t key, uint32_t d, uint32_t lane) {
-  const uint32_t row = key + 4u * (lane >> 5) + ((lane & 15u) >> 2), piece = d / 8u + 2u * ((lane >> 4) & 1u) + ((lane & 3u) >> 1);
+__device__ __forceinline__ half8 values(uint32_t at, uint32_t key, uint32_t d) {
   typedef __attribute__((address_space(3))) short4v* lds_ptr;
-  const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + row * (kPitch<DP> * 2) + ((piece ^ turn<DP>(row)) << 4) + (lane & 1u) * 8u));
-  const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + (row + 8u) * (kPitch<DP> * 2) + ((piece ^ turn<DP>(row + 8u)) << 4) + (lane & 1u) * 8u));
+  constexpr uint32_t kRow = kPitch<DP> * 2;
+  const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(uintptr_t)((at ^ (d << 1)) + key * kRow));
+  const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(uintptr_t)((at ^ (d << 1) ^ 32u) + (key + 8u) * kRow));
   return __builtin_bit_cast(half8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
@@ -186,35 +207,30 @@ __device__ __forceinline__ half8 weights(const float16v& s, int half) {
 }
 
 template <int DP, int B>
-__device__ __forceinline__ void add_values(Wave<DP>& w, const float16v (&s)[B], const uint8_t* tile, uint32_t lane) {
+__device__ __forceinline__ void add_values(Wave<DP>& w, const half8 (&p)[2 * B], uint32_t at) {
 #pragma unroll
-  for (int k = 0; k < 2 * B; ++k) {
-    const half8 p = weights(s[k / 2], k & 1);
+  for (int k = 0; k < 2 * B; ++k)
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d) w.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(values<DP>(tile, k * 16u, d * 32u, lane), p, w.o[d], 0, 0, 0);
-  }
+    for (int d = 0; d < DP / 32; ++d) w.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(values<DP>(at, k * 16u, d * 32u), p[k], w.o[d], 0, 0, 0);
 }
 
 // Does V in LDS hold an infinity or NaN?
 template <int DP, int ROWS>
-__device__ __forceinline__ bool any_not_finite(const uint8_t* tile, uint32_t lane) {
-  bool found = false;
-#pragma unroll
+__device__ __forceinline__ bool any_not_finite(uint32_t tile, uint32_t lane) {
+  uint32_t most = 0;  // magnitudes of two values; those of fp16 are ordered as their bits are
+#pragma unroll 2
   for (int i = 0; i < ROWS * kPitch<DP> / 512; ++i) {
-    const half8 v = *(const half8*)(tile + (i * 64u + lane) * 16u);
+    const u32x4 v = *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)(tile + (i * 64u + lane) * 16u);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) found |= !(__builtin_fabsf16(v[e]) <= (_Float16)65504.f);
+    for (int e = 0; e < 4; ++e) most = max_u16(most, v[e] & 0x7fff7fffu);
   }
-  return __any(found);
+  return __any((most & 0xffffu) >= 0x7c00u || most >= 0x7c000000u);
 }
 
 // add_values where some queries do not see some keys whose values are not finite: a weight of 0 times those is NaN.  Query by query,
 // with the values that the query does not see taken as 0; 32 times the work, for tiles that any_not_finite finds.
 template <int DP, int B>
-__device__ __forceinline__ void add_seen_values(Wave<DP>& w, const float16v (&s)[B], const uint8_t* tile, int key0, uint32_t lane) {
-  half8 p[2 * B];
-#pragma unroll
-  for (int k = 0; k < 2 * B; ++k) p[k] = weights(s[k / 2], k & 1);
+__device__ __forceinline__ void add_seen_values(Wave<DP>& w, const half8 (&p)[2 * B], uint32_t at, int key0, uint32_t lane) {
 #pragma unroll 1
   for (uint32_t query = 0; query < 32u; ++query) {
     const int limit = __builtin_amdgcn_readlane(w.limit, query) - key0;
@@ -224,7 +240,7 @@ __device__ __forceinline__ void add_seen_values(Wave<DP>& w, const float16v (&s)
       float16v o = {};
 #pragma unroll
       for (int k = 0; k < 2 * B; ++k) {
-        half8 v = values<DP>(tile, k * 16u, d * 32u, lane);
+        half8 v = values<DP>(at, k * 16u, d * 32u);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           if ((int)(k / 2 * 32u + key_of((k & 1) * 8 + i, lane)) > limit) v[i] = (_Float16)0.f;
@@ -236,23 +252,26 @@ __device__ __forceinline__ void add_seen_values(Wave<DP>& w, const float16v (&s)
   }
 }
 
-// One tile of 32 B keys from key0 on (relative to the sequence), of which `nk` is the number of keys.
-template <int DP, int B, bool MASK>
-__device__ __forceinline__ void attend(Wave<DP>& w, const uint8_t* k_tile, const uint8_t* v_tile, int key0, float scale_log2, uint32_t lane) {
+// One tile of 32 B keys from key0 on (relative to the sequence).  MASK: some query may not see some of them; CHECK: nor their values, be they not finite.
+template <int DP, int B, bool MASK, bool CHECK>
+__device__ __forceinline__ void attend(Wave<DP>& w, uint32_t k_tile, uint32_t v_tile, int key0, float scale_log2, uint32_t lane) {
+  const uint32_t k_at = place_in(k_tile, key_place<DP>(lane)), v_at = place_in(v_tile, value_place<DP>(lane));
   float16v s[B];
+  scores<DP, B>(w, k_at, s);
+  if (MASK) {
 #pragma unroll
-  for (int b = 0; b < B; ++b) {
-    s[b] = scores<DP>(w, k_tile + b * 32 * kPitch<DP> * 2, lane);
-    if (MASK) {
+    for (int b = 0; b < B; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (key0 + (int)(b * 32u + key_of(i, lane)) > w.limit) s[b][i] = -kInf;
-    }
   }
   settle<DP, B>(w, s, scale_log2);
   soften<DP, B>(w, s, scale_log2);
-  if (MASK && any_not_finite<DP, 32 * B>(v_tile, lane)) add_seen_values<DP, B>(w, s, v_tile, key0, lane);
-  else add_values<DP, B>(w, s, v_tile, lane);
+  half8 p[2 * B];
+#pragma unroll
+  for (int k = 0; k < 2 * B; ++k) p[k] = weights(s[k / 2], k & 1);
+  if (CHECK && any_not_finite<DP, 32 * B>(v_tile, lane)) add_seen_values<DP, B>(w, p, v_at, key0, lane);
+  else add_values<DP, B>(w, p, v_at);
 }
 
 // 32 d of a lane's query: four in a row at 8 a + 4 (l >> 5)
@@ -277,6 +296,17 @@ __device__ __forceinline__ float log_sum(float m, float l) { return l > 0.f ? (m
 
 constexpr uint32_t kTileQ = 128, kTileKeys = 64;
 
+// x of all lanes up to this one.
+__device__ __forceinline__ uint32_t sum_up_to_lane(uint32_t x) {
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);  // the lane before, in rows of 16
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);  // the last lane of the row before, for every second row
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);  // lane 31, for the upper half
+  return x;
+}
+
 template <int DP>
 __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
   constexpr int kBytes = kTileKeys * kPitch<DP> * 2;
@@ -284,21 +314,36 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t unit;
   if (!xcd_unit(p.units, unit)) return;
-  // head by head, so that what runs at one time on an XCD reads the same keys; the last queries, which see the most keys, first
+  // head by head, so that what runs at one time on an XCD reads the same keys
   const uint32_t whole = divide(unit, p.by_chunks), c = unit - whole * p.chunks;
-  const uint32_t head = divide(whole, p.by_slots), slot = p.slots - 1u - (whole - head * p.slots);
-  // sequence b has the slots from q_start[b] / 128 + b on: at least one for each 128 of its queries
-  uint32_t b = 0;
-  for (uint32_t at = 0; at < p.sequences; at += 64u) {
-    const uint32_t i = at + lane;
-    const bool begun = i < p.sequences && (uint32_t)p.q_start[i] / kTileQ + i <= slot;
-    b += __popcll(__ballot(begun));
+  const uint32_t head = divide(whole, p.by_slots), slot = whole - head * p.slots;
+  // Slots are counted over the sequences, one for each 128 queries; those left over lie at the end of a head.  (Slots that can be told from
+  // q_start alone, with one to spare for each sequence, left every second one empty for sequences of 128: the CUs that the hardware gives those to had half the
+  // work, and 64 such sequences took twice as long.)  A lane looks at one sequence; what is known of the one that has the slot comes from its lane.
+  Sequence s = {0, 0, 0u, 0u};
+  uint32_t passed = 0, first = 0;
+  bool found = false;
+  for (uint32_t at = 0; at < p.sequences && !found; at += 64u) {
+    Sequence mine = sequence(p, min(at + lane, p.sequences - 1u));
+    if (at + lane >= p.sequences) mine.nq = 0u;
+    const uint32_t has = (mine.nq + kTileQ - 1u) / kTileQ, upto = passed + sum_up_to_lane(has);
+    const uint64_t in = __ballot(slot >= upto - has && slot < upto);
+    found = in != 0ull;
+    if (found) {
+      const uint32_t l = (uint32_t)__builtin_ctzll(in);
+      s.q0 = (int32_t)__builtin_amdgcn_readlane((uint32_t)mine.q0, l);
+      s.k0 = (int32_t)__builtin_amdgcn_readlane((uint32_t)mine.k0, l);
+      s.nq = __builtin_amdgcn_readlane(mine.nq, l);
+      s.nk = __builtin_amdgcn_readlane(mine.nk, l);
+      // The last queries of a sequence, which see the most keys, come first.  Workgroups go to the four shader engines of an XCD in turn, whatever these
+      // have to do: every second four slots are taken backwards, or the first engine always had the longest of four (8 sequences of 1024: 8 % slower).
+      const uint32_t end = __builtin_amdgcn_readlane(upto, l), begin = end - __builtin_amdgcn_readlane(has, l), four = slot & ~3u;
+      const uint32_t turned = (slot & 4u) == 0u ? slot : max(four, begin) + min(four + 4u, end) - 1u - slot;
+      first = (end - 1u - turned) * kTileQ;
+    }
+    passed = __builtin_amdgcn_readlane(upto, 63);
   }
-  if (b == 0u) return;
-  --b;
-  const Sequence s = sequence(p, b);
-  const uint32_t first = (slot - ((uint32_t)p.q_start[b] / kTileQ + b)) * kTileQ;
-  if (first >= s.nq) return;
+  if (!found) return;
   const int off = (int)s.nk - (int)s.nq;  // query i sees keys up to i + off
 
   Wave<DP> w;
@@ -310,7 +355,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
 
   const int last = (int)min(first + kTileQ, s.nq) - 1 + off;  // last key that the workgroup's last query sees,
   const int low = (int)first + off;                           // its first query,
-  const int high = min((int)(first + wave * 32u) + 31, (int)s.nq - 1) + off;  // the wave's last query
+  const int wave_low = low + (int)wave * 32, high = min(wave_low + 31, (int)s.nk - 1);  // the wave's first and last
   const uint32_t keys = last < 0 ? 0u : (uint32_t)last + 1u;
   uint32_t t0 = 0, t1 = (keys + kTileKeys - 1) / kTileKeys;
   if (p.chunks > 1u) {
@@ -318,43 +363,79 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
     t0 = c * (p.chunk / kTileKeys);
     t1 = min(t1, t0 + p.chunk / kTileKeys);
   }
-  const uint32_t full = low < 0 ? 0u : ((uint32_t)low + 1u) / kTileKeys;  // tiles that all see
+  const uint32_t full = low < 0 ? 0u : ((uint32_t)low + 1u) / kTileKeys;  // tiles that all see (the same for all waves)
   auto issue = [&](uint32_t t, uint32_t to) {
     const int64_t row = s.k0 + (int64_t)t * kTileKeys;
     const uint32_t left = s.nk - t * kTileKeys;
     stage<DP, kTileKeys, 256>(p.K + row * p.k_row + (int64_t)g * p.k_head, p.k_row, left, p.dim, to, threadIdx.x);
     stage<DP, kTileKeys, 256>(p.V + row * p.v_row + (int64_t)g * p.v_head, p.v_row, left, p.dim, to + kBytes, threadIdx.x);
   };
-  uint32_t t = t0, now = 0;
   const uint32_t lds = lds_at(stages);
-  auto begin = [&]() {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's pieces of the tile are in LDS
-    __syncthreads();                                  // everybody's are, and nobody reads the other stage any more
-    if (t + 1u < t1) issue(t + 1u, lds + (now ^ 1u) * 2u * kBytes);
-  };
-  if (t < t1) issue(t, lds);
+  if (t0 < t1) issue(t0, lds);
   w.load(p.Q + (s.q0 + mine) * p.q_row + (int64_t)head * p.q_head, here, p.dim, lane);
   __builtin_amdgcn_s_waitcnt(0);  // the compiler's loads have come: it has nothing to wait for among the loop's
-  for (; t < min(full, t1); ++t, now ^= 1u) {
-    begin();
-    attend<DP, 2, false>(w, stages[now], stages[now] + kBytes, (int)(t * kTileKeys), p.scale_log2, lane);
-  }
-  for (; t < t1; ++t, now ^= 1u) {
-    begin();
-#pragma unroll 1
-    for (uint32_t half = 0; half < 2u; ++half) {  // half a tile at a time: with a mask, a whole one needs more registers than there are
-      const int key0 = (int)(t * kTileKeys + half * 32u);
-      if (key0 <= high) attend<DP, 1, true>(w, stages[now] + half * (kBytes / 2), stages[now] + kBytes + half * (kBytes / 2), key0, p.scale_log2, lane);
+  for (bool careful = false;; careful = true) {
+    uint32_t t = t0, now = 0;
+    auto begin = [&]() {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's pieces of the tile are in LDS
+      __syncthreads();                                  // everybody's are, and nobody reads the other stage any more
+      if (t + 1u < t1) issue(t + 1u, lds + (now ^ 1u) * 2u * kBytes);
+    };
+    for (; t < min(full, t1); ++t, now ^= 1u) {
+      begin();
+      const uint32_t at = lds + now * 2u * kBytes;
+      attend<DP, 2, false, false>(w, at, at + kBytes, (int)(t * kTileKeys), p.scale_log2, lane);
     }
+    for (; t < t1; ++t, now ^= 1u) {
+      begin();
+      const uint32_t at = lds + now * 2u * kBytes;
+      const int key0 = (int)(t * kTileKeys);
+      if (key0 > high) continue;
+      if (key0 + (int)kTileKeys - 1 <= wave_low) {
+        attend<DP, 2, false, false>(w, at, at + kBytes, key0, p.scale_log2, lane);
+      } else if (!careful) {
+        attend<DP, 2, true, false>(w, at, at + kBytes, key0, p.scale_log2, lane);
+      } else {
+#pragma unroll 1
+        for (uint32_t half = 0; half < 2u; ++half)
+          attend<DP, 1, true, true>(w, at + half * (kBytes / 2), at + kBytes + half * (kBytes / 2), key0 + (int)half * 32, p.scale_log2, lane);
+      }
+    }
+    // Sums that are not finite may come from values that a query does not see, times a weight of 0.  That is found here, once, and then all is done again with
+    // an eye on them: to look at every tile's values cost a tenth of short prompts.
+    float most = 0.f;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) most = fmaxf(most, w.o[d][i] - w.o[d][i] == 0.f ? 0.f : 1.f);
+    if (careful || full >= t1 || !__syncthreads_or(most != 0.f)) break;
+    w.clear();
+    issue(t0, lds);
   }
   w.l = across(w.l, true);
-  if (!here) return;
   const int64_t row = s.q0 + mine;
   if (p.chunks == 1u) {
-    store_rows<DP>(w, p.O + row * p.o_row + (int64_t)head * p.o_head, w.l > 0.f ? 1.f / w.l : w.l, p.dim, lane);
-    if (p.lse && lane < 32u) p.lse[(int64_t)head * p.q_rows + row] = log_sum(w.m, w.l);
+    // Through LDS, so that 16 (8) lanes write a row: stores of the 8 bytes that a lane has of its query took a seventh of short prompts' time.
+    __syncthreads();  // nobody reads a tile any more
+    constexpr uint32_t kRow = kPitch<DP> * 2, kPieces = kPitch<DP> / 8;
+    const uint32_t mine_at = lds + wave * 32u * kRow;
+    const float factor = w.l > 0.f ? 1.f / w.l : w.l;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int a = 0; a < 4; ++a)
+        *(__attribute__((address_space(3))) half4*)(uintptr_t)(mine_at + (lane & 31u) * kRow + (((d * 4u + a) ^ (lane & (kPieces - 1u))) << 4) + (lane >> 5) * 8u) =
+            half4{(_Float16)(w.o[d][4 * a] * factor), (_Float16)(w.o[d][4 * a + 1] * factor), (_Float16)(w.o[d][4 * a + 2] * factor), (_Float16)(w.o[d][4 * a + 3] * factor)};
+#pragma unroll
+    for (uint32_t i = 0; i < 32u * kPieces / 64u; ++i) {
+      const uint32_t r = i * (64u / kPieces) + lane / kPieces, piece = lane % kPieces, query = first + wave * 32u + r;
+      const half8 v = *(lds_half8)(uintptr_t)(mine_at + r * kRow + ((piece ^ (r & (kPieces - 1u))) << 4));
+      if (query < s.nq && piece * 8u < p.dim) *(half8*)(p.O + (s.q0 + query) * p.o_row + (int64_t)head * p.o_head + piece * 8u) = v;
+    }
+    if (here && p.lse && lane < 32u) p.lse[(int64_t)head * p.q_rows + row] = log_sum(w.m, w.l);
     return;
   }
+  if (!here) return;
   const uint64_t at = ((uint64_t)c * p.part_rows + row) * p.heads + head;
   float* out = p.part_o + at * DP;
 #pragma unroll
@@ -373,13 +454,13 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
 // a chunk of a sequence's keys, its waves take tiles of 32 in turn, each with two stages of its own in LDS and no barrier, and add
 // up what they have at the end.
 
-constexpr uint32_t kFewWaves = 2, kFewKeys = 32;
+constexpr uint32_t kFewKeys = 32;
 
-template <int DP>
-__global__ __launch_bounds__(kFewWaves * 64) void attention_few_kernel(AttentionParams p) {
+template <int DP, uint32_t WAVES>
+__global__ __launch_bounds__(WAVES * 64) void attention_few_kernel(AttentionParams p) {
   constexpr int kBytes = kFewKeys * kPitch<DP> * 2;
-  __shared__ __align__(16) uint8_t stage0[kFewWaves][2 * kBytes], stage1[kFewWaves][2 * kBytes];
-  __shared__ float top[kFewWaves][32], sum[kFewWaves][32];
+  __shared__ __align__(16) uint8_t stage0[WAVES][2 * kBytes], stage1[WAVES][2 * kBytes];
+  __shared__ float top[WAVES][32], sum[WAVES][32];
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // chunk outermost: sequences of one length run side by side
   const uint32_t kv_heads = p.heads / p.rep;
@@ -410,17 +491,17 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_few_kernel(Attention
     stage<DP, kFewKeys, 64>(K + (int64_t)key * p.k_row, p.k_row, left, p.dim, to, lane);
     stage<DP, kFewKeys, 64>(V + (int64_t)key * p.v_row, p.v_row, left, p.dim, to + kBytes, lane);
   };
-  constexpr uint32_t kStep = kFewWaves * kFewKeys;
-  auto tile = [&](uint32_t key, const uint8_t* at, uint32_t lds) {
+  constexpr uint32_t kStep = WAVES * kFewKeys;
+  auto tile = [&](uint32_t key, uint32_t at) {
     // all but the other stage's loads, which were issued after this one's
     if (kPitch<DP> == 128) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
     else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
     if (key < end) {
-      if ((int)(key + kFewKeys) - 1 <= low) attend<DP, 1, false>(w, at, at + kBytes, (int)key, p.scale_log2, lane);
-      else attend<DP, 1, true>(w, at, at + kBytes, (int)key, p.scale_log2, lane);
+      if ((int)(key + kFewKeys) - 1 <= low) attend<DP, 1, false, false>(w, at, at + kBytes, (int)key, p.scale_log2, lane);
+      else attend<DP, 1, true, true>(w, at, at + kBytes, (int)key, p.scale_log2, lane);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile has been read
-    issue(key + 2u * kStep, lds);
+    issue(key + 2u * kStep, at);
   };
   uint32_t key = begin + wave * kFewKeys;
   const uint32_t lds0 = lds_at(stage0[wave]), lds1 = lds_at(stage1[wave]);
@@ -428,8 +509,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_few_kernel(Attention
   issue(key, lds0);
   issue(key + kStep, lds1);
   for (; key < end; key += 2u * kStep) {
-    tile(key, stage0[wave], lds0);
-    tile(key + kStep, stage1[wave], lds1);
+    tile(key, lds0);
+    tile(key + kStep, lds1);
   }
   __builtin_amdgcn_s_waitcnt(0);  // no load into LDS is left
   __syncthreads();
@@ -440,12 +521,12 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_few_kernel(Attention
   __syncthreads();
   float m = top[0][lane & 31u];
 #pragma unroll
-  for (uint32_t i = 1; i < kFewWaves; ++i) m = fmaxf(m, top[i][lane & 31u]);
+  for (uint32_t i = 1; i < WAVES; ++i) m = fmaxf(m, top[i][lane & 31u]);
   const float down = w.m == -kInf ? 0.f : __builtin_amdgcn_exp2f(w.m - m);
   if (lane < 32u) sum[wave][lane] = w.l * down;
   // [wave][d / 4][query][4], in the stages' place
   float* all = (float*)stage0;
-  static_assert(sizeof(stage0) >= sizeof(float) * (kFewWaves - 1) * 32 * DP, "fits");
+  static_assert(sizeof(stage0) >= sizeof(float) * (WAVES - 1) * 32 * DP, "fits");
   if (wave != 0u) {
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
@@ -460,7 +541,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_few_kernel(Attention
   if (wave != 0u || !here) return;
   float l = sum[0][lane & 31u];
 #pragma unroll
-  for (uint32_t i = 1; i < kFewWaves; ++i) l += sum[i][lane & 31u];
+  for (uint32_t i = 1; i < WAVES; ++i) l += sum[i][lane & 31u];
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
@@ -469,7 +550,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_few_kernel(Attention
 #pragma unroll
       for (int e = 0; e < 4; ++e) w.o[d][4 * a + e] *= down;
 #pragma unroll
-      for (uint32_t i = 1; i < kFewWaves; ++i) {
+      for (uint32_t i = 1; i < WAVES; ++i) {
         const float4v other = *(const float4v*)(all + (((i - 1u) * (DP / 4) + quad) * 32u + (lane & 31u)) * 4u);
 #pragma unroll
         for (int e = 0; e < 4; ++e) w.o[d][4 * a + e] += other[e];
@@ -495,34 +576,55 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_few_kernel(Attention
 }
 
 // --- chunks joined --------------------------------------------------------------------------------------------------------------
-// A block has a query row and 8 or 16 heads; four d to a lane.  Chunks are added in their order.
-template <int DP>
+// 32 lanes have four d each of a query row and head, LANES of them side by side every LANES-th chunk; a block has 8 / LANES rows and heads.  The largest m
+// of all chunks comes first, so that no load waits for another one's result.  Sums are added in a fixed order.
+template <int DP, int LANES>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p) {
-  const uint32_t lane = threadIdx.x & 63u;
-  const int64_t row = blockIdx.x;
+  __shared__ float4v sum_o[8][32];
+  __shared__ float sum_l[8];
+  const uint32_t lane = threadIdx.x & 63u, part = threadIdx.x >> 5, mine = part % LANES;
+  const uint32_t pair = blockIdx.x * (8u / LANES) + part / LANES;  // the same for a wave
+  const uint32_t part_row = divide(pair, p.by_heads), head = pair - part_row * p.heads, d = (threadIdx.x & 31u) * 4u;
   uint32_t b = 0;
-  for (uint32_t at = 0; at < p.sequences; at += 64u) {
-    const uint32_t i = at + lane;
-    b += __popcll(__ballot(i < p.sequences && p.q_start[i] <= row));
+  if (p.few) {
+    b = divide(part_row, p.by_max_q) + 1u;
+  } else {
+    for (uint32_t at = 0; at < p.sequences; at += 64u) {
+      const uint32_t i = at + lane;
+      b += __popcll(__ballot(i < p.sequences && p.q_start[min(i, p.sequences - 1u)] <= (int64_t)part_row));
+    }
   }
-  const uint32_t head = blockIdx.y * (1024u / kPitch<DP>) + threadIdx.x / (kPitch<DP> / 4), d = threadIdx.x % (kPitch<DP> / 4) * 4u;
-  if (b == 0u || head >= p.heads || d >= (uint32_t)DP) return;
-  const Sequence s = sequence(p, b - 1u);
-  if (row < s.q0 || row >= s.q0 + s.nq) return;
-  const uint32_t n = min((s.nk + p.chunk - 1u) / p.chunk, p.chunks);
-  const uint64_t part_row = p.few ? (uint64_t)(b - 1u) * p.max_q + (uint64_t)(row - s.q0) : (uint64_t)row;
-  float m = -kInf, l = 0.f;
+  Sequence s = {0, 0, 0u, 0u};
+  if (b > 0u && part_row < p.part_rows) s = sequence(p, b - 1u);
+  const int64_t row = p.few ? s.q0 + (part_row - (b - 1u) * p.max_q) : (int64_t)part_row;
+  const bool there = row >= s.q0 && row < s.q0 + s.nq;
+  const uint32_t n = there ? min((s.nk + p.chunk - 1u) / p.chunk, p.chunks) : 0u;
+  const uint64_t first = (uint64_t)part_row * p.heads + head, step = p.part_rows * p.heads;
+  float m = -kInf;
+#pragma unroll 4
+  for (uint32_t c = 0; c < n; ++c) m = fmaxf(m, p.part_ml[(first + c * step) * 2]);
+  float l = 0.f;
   float4v o = {0.f, 0.f, 0.f, 0.f};
-  for (uint32_t c = 0; c < n; ++c) {
-    const uint64_t at = ((uint64_t)c * p.part_rows + part_row) * p.heads + head;
-    const float mc = p.part_ml[at * 2], lc = p.part_ml[at * 2 + 1];
-    const float4v oc = *(const float4v*)(p.part_o + at * DP + d);
-    if (mc == -kInf && lc == 0.f) continue;  // the query sees no key of the chunk
-    const float top = fmaxf(m, mc), old = m == -kInf ? 0.f : __builtin_amdgcn_exp2f(m - top), now = __builtin_amdgcn_exp2f(mc - top);
-    l = l * old + lc * now;
-    o = o * old + oc * now;
-    m = top;
+#pragma unroll 4
+  for (uint32_t c = mine; c < n; c += LANES) {
+    const float mc = p.part_ml[(first + c * step) * 2], lc = p.part_ml[(first + c * step) * 2 + 1];
+    const float4v oc = d < (uint32_t)DP ? *(const float4v*)(p.part_o + (first + c * step) * DP + d) : float4v{0.f, 0.f, 0.f, 0.f};
+    const float down = mc == -kInf ? 0.f : __builtin_amdgcn_exp2f(mc - m);  // a chunk of which the query sees no key: its l and o are 0 (or NaN, which stays)
+    l += lc * down;
+    o += oc * down;
   }
+  if (LANES > 1) {
+    sum_o[part][threadIdx.x & 31u] = o;
+    if (d == 0u) sum_l[part] = l;
+    __syncthreads();
+    if (mine != 0u) return;
+#pragma unroll
+    for (int i = 1; i < LANES; ++i) {
+      l += sum_l[part + i];
+      o += sum_o[part + i][threadIdx.x & 31u];
+    }
+  }
+  if (!there) return;
   if (d == 0u && p.lse) p.lse[(int64_t)head * p.q_rows + row] = log_sum(m, l);
   if (d >= p.dim) return;
   const float factor = l > 0.f ? 1.f / l : l;
@@ -541,7 +643,7 @@ AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads,
   plan.row_blocks = (uint32_t)((packed + 31) / 32);
   // workgroups with work if the keys are not split: about
   const uint64_t busy = plan.few ? (uint64_t)sequences * kv_heads * plan.row_blocks : ((uint64_t)q_rows + kTileQ - 1) / kTileQ * heads;
-  const uint64_t wanted = (plan.few ? 1024u : 512u) / (busy ? busy : 1), most = ((uint64_t)max_k + 255) / 256;
+  const uint64_t wanted = (plan.few ? 1024u : 256u) / (busy ? busy : 1), most = ((uint64_t)max_k + 255) / 256;
   uint64_t chunks = wanted < most ? wanted : most;
   if (chunks < 1) chunks = 1;
   plan.chunk = (uint32_t)((((uint64_t)max_k + chunks - 1) / chunks + 127) / 128 * 128);
@@ -557,11 +659,14 @@ AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads,
 
 template <int DP>
 static hipError_t run(AttentionParams& p, const AttentionPlan& plan, hipStream_t stream) {
-  if (plan.few) attention_few_kernel<DP><<<p.units, kFewWaves * 64, 0, stream>>>(p);
+  if (plan.few && p.units <= 256u) attention_few_kernel<DP, 4><<<p.units, 256, 0, stream>>>(p);
+  else if (plan.few) attention_few_kernel<DP, 2><<<p.units, 128, 0, stream>>>(p);
   else attention_kernel<DP><<<(p.units + 7u) / 8u * 8u, 256, 0, stream>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.chunks == 1u) return e;
-  attention_join_kernel<DP><<<dim3((uint32_t)p.q_rows, (p.heads + 1024 / kPitch<DP> - 1) / (1024 / kPitch<DP>)), 256, 0, stream>>>(p);
+  const uint64_t pairs = p.part_rows * p.heads;
+  if (p.chunks <= 2u) attention_join_kernel<DP, 2><<<(uint32_t)((pairs + 3u) / 4u), 256, 0, stream>>>(p);
+  else attention_join_kernel<DP, 8><<<(uint32_t)pairs, 256, 0, stream>>>(p);
   return hipGetLastError();
 }
 
@@ -579,6 +684,7 @@ hipError_t launch_attention(const AttentionLaunch& a, const AttentionPlan& plan,
   p.part_ml = a.parts + plan.chunks * plan.part_rows * a.heads * DP;
   p.part_rows = plan.part_rows;
   p.few = plan.few;
+  p.by_heads = divisor(a.heads), p.by_max_q = divisor((uint32_t)a.max_q);
   p.by_rep = divisor(p.rep), p.by_chunks = divisor(p.chunks), p.by_kv_heads = divisor(a.kv_heads);
   p.row_blocks = plan.row_blocks, p.slots = plan.slots, p.units = (uint32_t)plan.units;
   p.by_row_blocks = divisor(plan.few ? p.row_blocks : 1u), p.by_slots = divisor(p.slots);

@@ -12,6 +12,7 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTileM = 128;               // rows of a tile (one row band)
 constexpr int kTileK = 32;                // K extent of a tile = K of one 16x16x32 MFMA
@@ -34,6 +35,12 @@ __device__ __forceinline__ uint32_t scatter_addr(uint32_t word, uint32_t base) {
   uint32_t addr;
   asm("v_mad_u32_u16 %0, %1, 2, %2" : "=v"(addr) : "v"(word), "v"(base));
   return addr;
+}
+
+// The larger of two 16-bit numbers, twice.
+__device__ __forceinline__ uint32_t max_u16(uint32_t a, uint32_t b) {
+  const u16x2 x = __builtin_bit_cast(u16x2, a), y = __builtin_bit_cast(u16x2, b);
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, y));
 }
 
 // Where an array lies in LDS.

@@ -12,7 +12,6 @@
 namespace fls {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr uint32_t kBlock = 128;             // k that share a scale = K of one MFMA
@@ -20,11 +19,6 @@ constexpr uint32_t kPanel = 4;               // tile columns of a panel
 constexpr uint32_t kNowhere = 0x80000000u;   // an offset past every buffer descriptor here: a load from it gives 0
 
 // --- quantising a block -----------------------------------------------------------------------------------------------------
-
-__device__ __forceinline__ uint32_t max_u16(uint32_t a, uint32_t b) {
-  const u16x2 x = __builtin_bit_cast(u16x2, a), y = __builtin_bit_cast(u16x2, b);
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, y));
-}
 
 // Largest magnitude of 16 fp16 values, as bits; magnitudes of fp16 are ordered as their bits are.
 __device__ __forceinline__ uint32_t largest_bits(const u32x4& a, const u32x4& b) {
