@@ -363,12 +363,15 @@ def fls_quantize(W, out=None):
     assert W.is_cuda and W.dtype == torch.float16 and W.is_contiguous() and W.dim() == 2
     M, K = W.shape
     if out is None:
-        out = (torch.empty((M, K), dtype=torch.float8_e4m3fn, device=W.device),
-               torch.empty((M, scale_stride(K)), dtype=torch.float8_e8m0fnu, device=W.device))
-    Wq, Ws = out
-    assert Wq.is_cuda and Wq.dtype == torch.float8_e4m3fn and Wq.is_contiguous() and Wq.shape == (M, K)
-    assert Ws.is_cuda and Ws.dtype == torch.float8_e8m0fnu and Ws.is_contiguous() and Ws.shape == (M, scale_stride(K))
-    _check(lib().fls_quantize(W.data_ptr(), M, K, Wq.data_ptr(), Ws.data_ptr(), _stream()), "fls_quantize")
+        Wq = torch.empty_like(W, dtype=torch.float8_e4m3fn)
+        Ws = W.new_empty((M, scale_stride(K)), dtype=torch.float8_e8m0fnu)
+    else:
+        Wq, Ws = out
+        assert Wq.is_cuda and Wq.dtype == torch.float8_e4m3fn and Wq.is_contiguous() and Wq.shape == (M, K)
+        assert Ws.is_cuda and Ws.dtype == torch.float8_e8m0fnu and Ws.is_contiguous() and Ws.shape == (M, scale_stride(K))
+    rc = lib().fls_quantize(W.data_ptr(), M, K, Wq.data_ptr(), Ws.data_ptr(), _stream())
+    if rc != OK:
+        _check(rc, "fls_quantize")
     return Wq, Ws
 
 
@@ -387,7 +390,9 @@ def _ensure(need, where):
 
 def ensure_fp8_workspace(M, K, N):
     """ensure_workspace for fls_fp8_gemm."""
-    _ensure(fls_fp8_workspace_bytes(M, K, N), "fls_fp8_workspace_bytes")
+    need = lib().fls_fp8_workspace_bytes(M, K, N)
+    if need == 0 or _ws_tensor is None or _ws_tensor.numel() < need:
+        _ensure(need, "fls_fp8_workspace_bytes")
 
 
 def _fp8_args(Wq, Ws, X, C, M, K, N):
@@ -402,7 +407,9 @@ def _fp8_args(Wq, Ws, X, C, M, K, N):
 
 def fls_fp8_gemm(Wq, Ws, X, C, M, K, N):
     """C = W . X with W as fls_quantize returned it; X float16 [N, K], C float16 [N, M] as everywhere."""
-    _check(lib().fls_fp8_gemm(*_fp8_args(Wq, Ws, X, C, M, K, N)), "fls_fp8_gemm")
+    rc = lib().fls_fp8_gemm(*_fp8_args(Wq, Ws, X, C, M, K, N))
+    if rc != OK:
+        _check(rc, "fls_fp8_gemm")
     return C
 
 
@@ -420,50 +427,60 @@ def prepare_fp8_gemm(Wq, Ws, X, C, M, K, N):
 
 
 _ATTENTION_LAYOUT = struct.Struct("<10q4i2qf4x")  # fls_attention_shape
+_pack_attention = _ATTENTION_LAYOUT.pack
 
 
-def _attention_shape(Q, K, V, O, sequences, max_q, max_k, scale):
-    (q_rows, heads, dim), (k_rows, kv_heads, _) = Q.shape, K.shape
-    q, k, v, o = Q.stride(), K.stride(), V.stride(), O.stride()
-    q0, k0, v0, o0 = (q[0], k[0], v[0], o[0]) if q_rows > 1 and k_rows > 1 else (  # the stride of one row or head says nothing
-        q_rows > 1 and q[0], k_rows > 1 and k[0], k_rows > 1 and v[0], q_rows > 1 and o[0])
-    q1, o1 = (q[1], o[1]) if heads > 1 else (0, 0)
-    k1, v1 = (k[1], v[1]) if kv_heads > 1 else (0, 0)
-    return _ATTENTION_LAYOUT.pack(q_rows, k_rows, q0, q1, k0, k1, v0, v1, o0, o1, sequences, heads, kv_heads, dim, max_q, max_k, scale)
+def _attention_workspace_bytes(q_rows, heads, dim, k_rows, kv_heads, sequences, max_q, max_k):
+    # strides do not matter here
+    return lib().fls_attention_workspace_bytes(_pack_attention(q_rows, k_rows, 0, 0, 0, 0, 0, 0, heads * dim, dim, sequences, heads, kv_heads, dim, max_q, max_k, 1.0))
 
 
 def fls_attention_workspace_bytes(Q, K, sequences, max_q, max_k):
-    (q_rows, heads, dim), (k_rows, kv_heads, _) = Q.shape, K.shape  # strides do not matter here
-    return int(lib().fls_attention_workspace_bytes(_ATTENTION_LAYOUT.pack(q_rows, k_rows, 0, 0, 0, 0, 0, 0, heads * dim, dim, sequences, heads, kv_heads, dim,
-                                                                          max_q, max_k, 1.0)))
+    return int(_attention_workspace_bytes(*Q.shape, *K.shape[:2], sequences, max_q, max_k))
 
 
 def ensure_attention_workspace(Q, K, q_start, max_q, max_k):
     """ensure_workspace for fls_attention."""
-    _ensure(fls_attention_workspace_bytes(Q, K, q_start.shape[0] - 1, max_q, max_k), "fls_attention_workspace_bytes")
+    need = _attention_workspace_bytes(*Q.shape, *K.shape[:2], q_start.shape[0] - 1, max_q, max_k)
+    if need == 0 or _ws_tensor is None or _ws_tensor.numel() < need:
+        _ensure(need, "fls_attention_workspace_bytes")
 
 
 def _attention_args(Q, K, V, O, q_start, k_start, k_len, max_q, max_k, scale, lse):
     import torch
 
     f16, i32 = torch.float16, torch.int32
-    assert Q.is_cuda and Q.dtype == f16 and Q.dim() == 3 and Q.stride(2) == 1 and K.is_cuda and K.dtype == f16 and K.dim() == 3 and K.stride(2) == 1
-    assert V.is_cuda and V.dtype == f16 and V.shape == K.shape and V.stride(2) == 1 and O.is_cuda and O.dtype == f16 and O.shape == Q.shape and O.stride(2) == 1
-    assert K.shape[2] == Q.shape[2]
-    assert q_start.is_cuda and q_start.dtype == i32 and q_start.dim() == 1 and q_start.is_contiguous() and q_start.shape[0] > 0
-    sequences = q_start.shape[0] - 1
-    assert k_start.is_cuda and k_start.dtype == i32 and k_start.shape == (sequences,) and k_start.is_contiguous()
-    assert k_len.is_cuda and k_len.dtype == i32 and k_len.shape == (sequences,) and k_len.is_contiguous()
-    assert lse is None or (lse.is_cuda and lse.dtype == torch.float32 and lse.shape == (Q.shape[1], Q.shape[0]) and lse.is_contiguous())
-    return (Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), None if lse is None else lse.data_ptr(), q_start.data_ptr(), k_start.data_ptr(),
-            k_len.data_ptr(), _attention_shape(Q, K, V, O, sequences, max_q, max_k, scale), _stream())
+    q_rows, heads, dim = shape = Q.shape
+    k_rows, kv_heads, k_dim = k_shape = K.shape
+    (q0, q1, q2), (k0, k1, k2), (v0, v1, v2), (o0, o1, o2) = Q.stride(), K.stride(), V.stride(), O.stride()
+    sequences = k_len.shape[0]
+    assert Q.is_cuda and K.is_cuda and V.is_cuda and O.is_cuda and Q.dtype == f16 and K.dtype == f16 and V.dtype == f16 and O.dtype == f16
+    assert k_dim == dim and V.shape == k_shape and O.shape == shape and q2 == k2 == v2 == o2 == 1
+    assert q_start.is_cuda and k_start.is_cuda and k_len.is_cuda and q_start.dtype == i32 and k_start.dtype == i32 and k_len.dtype == i32
+    assert q_start.shape == (sequences + 1,) and k_start.shape == (sequences,) and q_start.is_contiguous() and k_start.is_contiguous() and k_len.is_contiguous()
+    if lse is not None:
+        assert lse.is_cuda and lse.dtype == torch.float32 and lse.shape == (heads, q_rows) and lse.is_contiguous()
+        lse = lse.data_ptr()
+    if q_rows <= 1:  # the stride of one row or one head says nothing
+        q0 = o0 = 0
+    if k_rows <= 1:
+        k0 = v0 = 0
+    if heads == 1:
+        q1 = o1 = 0
+    if kv_heads == 1:
+        k1 = v1 = 0
+    return (Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), lse, q_start.data_ptr(), k_start.data_ptr(), k_len.data_ptr(),
+            _pack_attention(q_rows, k_rows, q0, q1, k0, k1, v0, v1, o0, o1, sequences, heads, kv_heads, dim, max_q, max_k, scale), _stream())
 
 
 def fls_attention(Q, K, V, O, q_start, k_start, k_len, max_q, max_k, scale, lse=None):
     """Causal attention of packed sequences: Q, O float16 [rows, heads, head_dim], K, V float16 [rows, kv_heads, head_dim], any strides but a last
     one of 1 - slices of the QKV product's C, a cache.  q_start int32 [sequences + 1], k_start and k_len int32 [sequences], on the GPU: sequence b has
-    queries q_start[b] ... q_start[b + 1] - 1 and k_len[b] keys from row k_start[b] on, its last query sees all of them.  lse: float32 [heads, rows] or None."""
-    _check(lib().fls_attention(*_attention_args(Q, K, V, O, q_start, k_start, k_len, max_q, max_k, scale, lse)), "fls_attention")
+    queries q_start[b] ... q_start[b + 1] - 1 and k_len[b] keys from row k_start[b] on, its last query sees all of them.  max_q, max_k: the most queries and
+    keys that a sequence has, or more.  lse: float32 [heads, rows] or None."""
+    rc = lib().fls_attention(*_attention_args(Q, K, V, O, q_start, k_start, k_len, max_q, max_k, scale, lse))
+    if rc != OK:
+        _check(rc, "fls_attention")
     return O
 
 

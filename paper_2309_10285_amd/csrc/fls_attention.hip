@@ -72,7 +72,7 @@ __device__ __forceinline__ uint32_t turn(uint32_t row) {
 }
 
 // ROWS rows to LDS by THREADS lanes; rows from `left` on and values from dim on are 0.
-template <int DP, int ROWS, int THREADS>
+template <int DP, int ROWS, int THREADS, bool STREAM = false>
 __device__ __forceinline__ void stage(const _Float16* first, int64_t row_stride, uint32_t left, uint32_t dim, uint32_t lds, uint32_t thread) {
   constexpr uint32_t kPieces = kPitch<DP> / 8, kStep = THREADS / kPieces;  // rows to a load of all lanes
   static_assert(ROWS % kStep == 0 && (kStep % 16 == 0 || 16 % kStep == 0), "whole loads");
@@ -83,7 +83,7 @@ __device__ __forceinline__ void stage(const _Float16* first, int64_t row_stride,
   for (int i = 0; i < ROWS / (int)kStep; ++i) {
     const uint32_t row = i * kStep + thread / kPieces, piece = (thread % kPieces) ^ turn<DP>(row);
     const uint32_t off = row * (uint32_t)(row_stride * 2) + piece * 16u;
-    load_lds<16>(buf, lds + i * THREADS * 16 + wave * 1024u, row < left && piece * 8u < dim ? off : kNowhere);
+    load_lds<16, STREAM>(buf, lds + i * THREADS * 16 + wave * 1024u, row < left && piece * 8u < dim ? off : kNowhere);
   }
 }
 
@@ -450,7 +450,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
 }
 
 // --- few queries to a sequence -------------------------------------------------------------------------------------------------
-// Bound by the stream of keys and values.  The queries of all heads that share a key head are the 32 columns of a wave; a workgroup has
+// Bound by the stream of keys and values (loads that the caches do not keep: 64 tokens, 56 heads, 345 -> 313 us).  The queries of all heads that share a key head are the 32 columns of a wave; a workgroup has
 // a chunk of a sequence's keys, its waves take tiles of 32 in turn, each with two stages of its own in LDS and no barrier, and add
 // up what they have at the end.
 
@@ -479,7 +479,6 @@ __global__ __launch_bounds__(WAVES * 64) void attention_few_kernel(AttentionPara
   Wave<DP> w;
   const uint32_t packed = block * 32u + (lane & 31u), query = divide(packed, p.by_rep), head = g * p.rep + packed - query * p.rep;
   const bool here = packed < rows;
-  w.load(p.Q + (s.q0 + query) * p.q_row + (int64_t)head * p.q_head, here, p.dim, lane);
   w.limit = here ? (int)query + off : -1;
   w.clear();
   const int low = (int)divide(block * 32u, p.by_rep) + off;  // last key of the wave's first query
@@ -488,8 +487,8 @@ __global__ __launch_bounds__(WAVES * 64) void attention_few_kernel(AttentionPara
   const _Float16* V = p.V + s.k0 * p.v_row + (int64_t)g * p.v_head;
   auto issue = [&](uint32_t key, uint32_t to) {
     const uint32_t left = key < end ? end - key : 0u;
-    stage<DP, kFewKeys, 64>(K + (int64_t)key * p.k_row, p.k_row, left, p.dim, to, lane);
-    stage<DP, kFewKeys, 64>(V + (int64_t)key * p.v_row, p.v_row, left, p.dim, to + kBytes, lane);
+    stage<DP, kFewKeys, 64, true>(K + (int64_t)key * p.k_row, p.k_row, left, p.dim, to, lane);
+    stage<DP, kFewKeys, 64, true>(V + (int64_t)key * p.v_row, p.v_row, left, p.dim, to + kBytes, lane);
   };
   constexpr uint32_t kStep = WAVES * kFewKeys;
   auto tile = [&](uint32_t key, uint32_t at) {
@@ -505,9 +504,10 @@ __global__ __launch_bounds__(WAVES * 64) void attention_few_kernel(AttentionPara
   };
   uint32_t key = begin + wave * kFewKeys;
   const uint32_t lds0 = lds_at(stage0[wave]), lds1 = lds_at(stage1[wave]);
-  __builtin_amdgcn_s_waitcnt(0);  // the queries have come: the compiler has nothing to wait for among the loop's loads
   issue(key, lds0);
   issue(key + kStep, lds1);
+  w.load(p.Q + (s.q0 + query) * p.q_row + (int64_t)head * p.q_head, here, p.dim, lane);
+  __builtin_amdgcn_s_waitcnt(0);  // the queries have come: the compiler has nothing to wait for among the loop's loads
   for (; key < end; key += 2u * kStep) {
     tile(key, lds0);
     tile(key + kStep, lds1);
@@ -643,7 +643,7 @@ AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads,
   plan.row_blocks = (uint32_t)((packed + 31) / 32);
   // workgroups with work if the keys are not split: about
   const uint64_t busy = plan.few ? (uint64_t)sequences * kv_heads * plan.row_blocks : ((uint64_t)q_rows + kTileQ - 1) / kTileQ * heads;
-  const uint64_t wanted = (plan.few ? 1024u : 256u) / (busy ? busy : 1), most = ((uint64_t)max_k + 255) / 256;
+  const uint64_t wanted = (plan.few ? 512u : 256u) / (busy ? busy : 1), most = ((uint64_t)max_k + 255) / 256;
   uint64_t chunks = wanted < most ? wanted : most;
   if (chunks < 1) chunks = 1;
   plan.chunk = (uint32_t)((((uint64_t)max_k + chunks - 1) / chunks + 127) / 128 * 128);

@@ -55,12 +55,13 @@ __device__ __forceinline__ u32x4 descriptor(const void* p, uint64_t bytes) {
 // 16 (or 4) bytes to a lane straight to LDS at `lds` + 16 (4) lane (`lds` the same for the wave).  An asm statement, because the compiler waits for
 // loads into LDS that it knows of wherever it cannot tell what is read (a ring of stages, a transposing read), and at barriers, which would leave
 // nothing in flight.  It writes no register but m0, which nothing else in the kernels that use it needs (the compiler keeps nothing there);
-// who reads the LDS waits for it (vmcnt).
-template <int BYTES>
+// who reads the LDS waits for it (vmcnt).  STREAM: what is read once; the caches need not keep it.
+template <int BYTES, bool STREAM = false>
 __device__ __forceinline__ void load_lds(u32x4 buf, uint32_t lds, uint32_t off) {
   static_assert(BYTES == 16 || BYTES == 4, "");
   const uint32_t at = __builtin_amdgcn_readfirstlane(lds);
-  if (BYTES == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(buf) : "memory");
+  if (BYTES == 16 && STREAM) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(at), "v"(off), "s"(buf) : "memory");
+  else if (BYTES == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(buf) : "memory");
   else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(off), "s"(buf) : "memory");
 }
 

@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(const _Float16* W, uint8_
   if (FRAGMENTS) {
     const uint32_t piece = slot & 7u, step = slot >> 3;
     if (here && step * kBlock < K)
-      *(u32x4*)(q + (((uint64_t)step * columns + row / 16u) * 2u + piece / 4u) * 1024u + (piece % 4u * 16u + row % 16u) * 16u) = to_e4m3(a, b, byte);
+      *(u32x4*)(q + (((uint64_t)step * columns + row / 16u) * 2u + piece % 2u) * 1024u + (piece / 2u * 16u + row % 16u) * 16u) = to_e4m3(a, b, byte);
   } else if (in) {
     __builtin_nontemporal_store(to_e4m3(a, b, byte), (u32x4*)(q + row * K + k));
   }
@@ -129,11 +129,12 @@ __device__ __forceinline__ float4v mfma(const i32x8& a, const i32x8& b, const fl
 }
 
 // Up to 64 columns: bound by the stream of W.  A workgroup has 16 RB rows and a K slice; its waves take the slice's steps of 128 k in turn, so that they
-// read neighbouring 128 B lines of the same rows, straight into MFMA fragments (lane l: row l & 15, bytes 16 (l >> 4) .. + 15 and
-// the same 64 further: which k a lane contributes is free as long as X uses the same), a step ahead.  The waves' sums meet in LDS.
+// read neighbouring 128 B lines of the same rows, a step ahead.  A load takes whole lines, 8 rows of them, which the caches need not keep (lane l: row l & 7,
+// piece l >> 3 of 16 B); neighbours at a distance of 8 lanes then exchange a piece each, which leaves MFMA fragments: lane l has bytes 32 (l >> 4) .. + 31
+// of row l & 15.  (Loaded as fragments, two loads share every line: it has to stay in the caches for the second: 50257 x 7168, N = 13, 72 us, 65.5 so.)  The waves' sums meet in LDS.
 // What counts beside W's own loads is how many lines they ask for: the slice's scales of W are copied to LDS row by row (a byte of each row for every step,
-// as many lines again as half of W, cost 8 - 20 %), X lies in fragment order (from fp16 rows: 10 - 30 % more), and W's loads leave the line that two of them share in the
-// caches (not to: 10 %).  QUANT: a wave quantises the X that it multiplies itself, in registers, for calls where another kernel in front would cost more.
+// as many lines again as half of W, cost 8 - 20 %), and X lies in fragment order (from fp16 rows: 10 - 30 % more).
+// QUANT: a wave quantises the X that it multiplies itself, in registers, for calls where another kernel in front would cost more.
 // One step ahead and eight waves, four for 64 columns: a deeper ring or other numbers of waves were up to 5 % slower (of 28672 x 7168, N = 64: 53 us in
 // four, 56 in eight).
 constexpr int stream_waves(int NB) { return NB == 4 ? 4 : 8; }
@@ -153,8 +154,7 @@ __global__ __launch_bounds__(stream_waves(NB) * 64) void fp8_stream_kernel(Fp8Pa
   const uint32_t rows = min((uint32_t)kRows, p.M - row0);
   const __amdgpu_buffer_rsrc_t wbuf = buffer(p.W + (uint64_t)row0 * p.K, (uint64_t)rows * p.K);
   const __amdgpu_buffer_rsrc_t xbuf = QUANT ? buffer(p.X, (uint64_t)p.N * p.K * 2u) : buffer(p.Xq, (uint64_t)p.steps * (NB * 2048u));
-  const uint32_t r = lane & 15u, k_lane = (lane >> 4) * 16u;
-  const uint32_t w_off = r * p.K + k_lane;
+  const uint32_t r = lane & 15u, w_off = (lane & 7u) * p.K + (lane >> 3) * 16u;
 
   float4v acc[RB][NB];
 #pragma unroll
@@ -169,26 +169,41 @@ __global__ __launch_bounds__(stream_waves(NB) * 64) void fp8_stream_kernel(Fp8Pa
 
   // a step past the slice loads nothing (every offset is nowhere); of a K that is no multiple of 128 the last step has the lanes before K
   auto issue = [&](Stage& s, uint32_t step) {
-    const uint32_t k = step * kBlock + k_lane, k_end = step < step1 ? p.K : 0u;
-    const bool in0 = k < k_end, in1 = k + 64u < k_end;
+    const uint32_t k_end = step < step1 ? p.K : 0u;
+    const bool in = step * kBlock + (lane >> 3) * 16u < k_end;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const uint32_t at = w_off + rb * 16u * p.K + step * kBlock;
-      s.w[rb][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wbuf, in0 ? at : kNowhere, 0, 0));
-      s.w[rb][1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wbuf, in1 ? at + 64u : kNowhere, 0, 0));
-    }
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        s.w[rb][h] = __builtin_bit_cast(
+            u32x4, __builtin_amdgcn_raw_buffer_load_b128(wbuf, in ? w_off + (rb * 16u + h * 8u) * p.K + step * kBlock : kNowhere, 0, kAuxNonTemporal));
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int j = 0; j < XL; ++j) {
         uint32_t off;
-        if (QUANT) off = (j < XL / 2 ? in0 : in1) ? (((nb * 16u + r) * p.K + step * kBlock + k_lane) + (j / 2) * 64u + (j % 2) * 8u) * 2u : kNowhere;
+        const uint32_t k = step * kBlock + (lane >> 4) * 32u + j * 8u;
+        if (QUANT) off = k < k_end ? ((nb * 16u + r) * p.K + k) * 2u : kNowhere;
         else off = step < step1 ? ((step * NB + nb) * 2u + j) * 1024u + lane * 16u : kNowhere;
         s.x[nb][j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xbuf, off, 0, 0));
       }
   };
+  const bool upper = (lane & 8u) != 0u;
+  auto fragment = [&](const u32x4& a, const u32x4& b) {  // a: rows 0 - 7, b: rows 8 - 15
+    u32x4 first, second;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(upper ? a[i] : b[i]), 0x128, 0xf, 0xf, true);  // from the lane 8 further, in rows of 16
+      first[i] = upper ? other : a[i];
+      second[i] = upper ? b[i] : other;
+    }
+    return join(first, second);
+  };
   auto consume = [&](Stage& s, uint32_t step) {
     const uint8_t* scale = lds + step - step0;
+    i32x8 w[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) w[rb] = fragment(s.w[rb][0], s.w[rb][1]);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       i32x8 x;
@@ -209,7 +224,7 @@ __global__ __launch_bounds__(stream_waves(NB) * 64) void fp8_stream_kernel(Fp8Pa
         xs = scale[(kRows + nb * 16u + r) * kScalePitch];
       }
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) acc[rb][nb] = mfma(join(s.w[rb][0], s.w[rb][1]), x, acc[rb][nb], scale[(rb * 16u + r) * kScalePitch], xs);
+      for (int rb = 0; rb < RB; ++rb) acc[rb][nb] = mfma(w[rb], x, acc[rb][nb], scale[(rb * 16u + r) * kScalePitch], xs);
     }
   };
 
@@ -456,17 +471,18 @@ Fp8Plan fp8_plan(uint32_t M, uint32_t K, uint32_t N, int cus) {
   const uint64_t room = fp8_parts_bytes() / sizeof(float) / ((uint64_t)M * N);  // slices whose sums there is room for (0: one, with no sums)
   const uint32_t least_slices = (steps + kStreamSteps - 1) / kStreamSteps;
   if (N <= 64 && (least_slices == 1u || least_slices <= room)) {
-    // Streams run at 5.2 TB/s if every CU has as many workgroups as the others (c of them); with many, half a one is lost at the end.  16 and 32 rows to a workgroup
-    // read X more often than 64 do: 28672 x 7168, N = 13: 46, 42, 40 us, N = 32: 58, 49, 45, N = 64: 94, 68, 56.  12288 x 12288, N = 13:
-    // 31 us in two slices of 32 rows (c = 3), 36 in one of 64 (c = 3/4).
+    // Streams run at 5.6 TB/s.  c workgroups to a CU: up to two, some CUs have one more than others; more even out.  16 and 32 rows to a workgroup read X more
+    // often than 64 do - 28672 x 7168, N = 13: 41, 38, 36 us, N = 32: 45 and 40 us in 32 and 64 rows, N = 64: 60 and 48 - and where there is one to a CU they have
+    // fewer loads under way: 7168 x 28672, N = 13: 42 us in 32 rows, 39 in 64 and two slices.  12288 x 12288, N = 13: 30 us in four slices of 64 rows (c = 3), 36 in one (c = 3/4).
     const uint32_t nb = fp8_column_groups(N);
-    const float extra[3][3] = {{1.f, 1.02f, 1.2f}, {1.f, 1.08f, 1.25f}, {1.f, 1.2f, 1.5f}};
+    const float extra[3][3] = {{1.f, 1.02f, 1.15f}, {1.f, 1.12f, 1.3f}, {1.f, 1.22f, 1.5f}};
     for (int i = 0; i < 3; ++i)
       for (uint32_t slices = least_slices; slices <= least_slices + 7u; ++slices) {
-        if (slices > least_slices && (slices > room || slices * 8u > steps)) break;
+        if (slices > least_slices && (slices > room || slices * 16u > steps)) break;
         const uint32_t rows = 64u >> i;
-        const float c = (float)((M + rows - 1) / rows) * slices / cus, whole = ceilf(c);
-        const float us = (float)M * K / 5.2e6f * (c <= 4.f ? whole / c : (c + 0.5f) / c) * extra[nb / 2][i] + sums_us(slices, M, N);
+        const float c = (float)((M + rows - 1) / rows) * slices / cus, uneven = 0.88f * ceilf(c) / c;
+        const float us = (float)M * K / 5.6e6f * (c > 2.f ? 1.03f : uneven > 1.f ? uneven : 1.f) * extra[nb / 2][i] * (c <= 1.f ? 1.f + 0.12f * i : 1.f) +
+                         sums_us(slices, M, N);
         if (us < least) {
           least = us;
           best.tile_m = rows;
