@@ -215,8 +215,13 @@ def _run_layer_on_stream(args, torch, wl, fls, side):
     mats = wl.decoder_layer(7168, 28672, N, beta)
     fls.ensure_workspace(max(c.M for c in mats), max(c.K for c in mats), N)
     copies = 3
-    sparse, dense, recs = [], [], []
-    for cfg in mats:
+    sparse, dense, fp8, recs = [], [], [], []
+    attention = None
+    if args.layer_context:
+        attention = _layer_attention(args, torch, fls, N, copies)
+    if args.layer_fp8:
+        fls.ensure_fp8_workspace(max(c.M for c in mats), max(c.K for c in mats), N)
+    for i, cfg in enumerate(mats):
         W32 = wl.make_w32(cfg)
         Wb, Xb = wl.make_inputs(cfg, W32)
         X = torch.from_numpy(Xb.view(np.float16)).cuda()
@@ -229,6 +234,12 @@ def _run_layer_on_stream(args, torch, wl, fls, side):
         D = torch.empty((N, cfg.M), dtype=torch.float16, device="cuda")
         sparse.append([fls.prepare_spmm(b, X, C, cfg.M, cfg.K, N) for b in blobs])
         dense.append([fls.prepare_dense_gemm(w, X, D, cfg.M, cfg.K, N) for w in Wds])
+        if args.layer_fp8:
+            Wq, Ws = fls.fls_quantize(Wd)
+            E = torch.empty((N, cfg.M), dtype=torch.float16, device="cuda")
+            Wqs = [Wq] + [Wq.clone() for _ in range(copies - 1)]
+            fp8.append([fls.prepare_fp8_gemm(w, Ws, X, E, cfg.M, cfg.K, N) for w in Wqs])
+            fms, _ = _time_loop(fp8[-1], args.steps, args.warmup)
         ms, _ = _time_loop(sparse[-1], args.steps, args.warmup)
         dms, _ = _time_loop(dense[-1], args.steps, args.warmup)
         err = None
@@ -241,6 +252,15 @@ def _run_layer_on_stream(args, torch, wl, fls, side):
         recs.append({"matmul": cfg.what, "M": cfg.M, "K": cfg.K, "nnz": st["nnz"], "alone_us": round(ms * 1e3, 2),
                      "alone_GBps": round(alg / ms / 1e6, 1), "dense_alone_us": round(dms * 1e3, 2),
                      "algorithmic_bytes": alg, "max_rel_err_whole_c": err})
+        if args.layer_fp8:
+            recs[-1]["fp8_alone_us"] = round(fms * 1e3, 2)
+            # against the dense product of the same weights: both operands are rounded to 4 significant bits
+            recs[-1]["fp8_rel_err_vs_dense"] = float((E.double() - D.double()).norm() / D.double().norm())
+        if attention and i == 0:  # the step between the QKV product and the output projection, in all kinds of layer
+            calls = [attention[0](c) for c in range(copies)]
+            for table in (sparse, dense, fp8):
+                if table:
+                    table.append(calls)
 
     def layer_calls(table):
         return [lambda c=c, table=table: [calls[c]() for calls in table] for c in range(copies)]
@@ -256,24 +276,74 @@ def _run_layer_on_stream(args, torch, wl, fls, side):
     layer_steps = max(50, args.steps // 4)
     out = {"mode": "decoder layer", "model": "OPT-30B-shaped (hidden 7168, FFN 28672)", "N": N, "sparsity": beta,
            "weight_copies_rotated": copies, "layers_timed": layer_steps, "matmuls": recs}
-    for name, table in (("spmm", sparse), ("dense", dense)):
+    if attention:
+        out.update(attention[1]())
+    for name, table in (("spmm", sparse), ("dense", dense)) + ((("fp8", fp8),) if fp8 else ()):
         ms, _ = _time_loop(layer_calls(table), layer_steps, max(10, args.warmup // 4))
         out[f"{name}_layer_us_eager"] = round(ms * 1e3, 2)
         g = graph_of(table)
         gms, _ = _time_loop([g.replay], max(20, layer_steps // copies), 5)
         out[f"{name}_layer_us_graph"] = round(gms * 1e3 / copies, 2)
-    alg = sum(r["algorithmic_bytes"] for r in recs)
+    alg = sum(r["algorithmic_bytes"] for r in recs) + out.get("attention_bytes", 0)
     out["spmm_layer_GBps_graph"] = round(alg / out["spmm_layer_us_graph"] / 1e3, 1)
     out["spmm_layer_hbm_frac_graph"] = round(alg / out["spmm_layer_us_graph"] / 1e3 / HBM_PEAK_GBS, 4)
-    out["sum_of_alone_us"] = round(sum(r["alone_us"] for r in recs), 2)
+    out["sum_of_alone_us"] = round(sum(r["alone_us"] for r in recs) + out.get("attention_alone_us", 0.0), 2)
     out["layer_speedup_vs_dense_graph"] = round(out["dense_layer_us_graph"] / out["spmm_layer_us_graph"], 3)
     return out
 
 
+def _layer_attention(args, torch, fls, N, copies):
+    """Causal attention of one decode step: N sequences, each with args.layer_context keys in a slab of a cache (the
+    step's own key is the last), 56 heads of 128.  A step writes the new keys and values into the cache and attends.
+    Its queries, keys and values are a buffer of N(0, 1) with the strides of the QKV product's C: every product of
+    the timed layer has an input of its own, so that each can be checked.  Returns (step of a copy, record)."""
+    H, D, L = 56, 128, args.layer_context
+    gen = torch.Generator(device="cuda").manual_seed(0x5EED0070)
+
+    def randn(*shape):
+        return torch.randn(shape, generator=gen, device="cuda").half()
+
+    def ints(values):
+        return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+    qkv, O = randn(N, 3 * H, D), torch.empty((N, H, D), dtype=torch.float16, device="cuda")
+    caches = [(randn(N * L, H, D), randn(N * L, H, D)) for _ in range(copies)]
+    q_start, k_start, k_len = ints(list(range(N + 1))), ints([n * L for n in range(N)]), ints([L] * N)
+    Q = qkv[:, :H]
+    fls.ensure_attention_workspace(Q, caches[0][0], q_start, 1, L)
+    calls = [fls.prepare_attention(Q, k, v, O, q_start, k_start, k_len, 1, L, D ** -0.5) for k, v in caches]
+
+    def step(c):
+        k, v = (t.view(N, L, H, D)[:, L - 1] for t in caches[c])
+
+        def call():
+            k.copy_(qkv[:, H:2 * H])
+            v.copy_(qkv[:, 2 * H:])
+            calls[c]()
+
+        return call
+
+    def record():
+        for c in range(copies):
+            step(c)()
+        ms, _ = _time_loop(calls, args.steps, args.warmup)
+        calls[0]()
+        k, v = (t.view(N, L, H, D).float() for t in caches[0])
+        p = torch.softmax((k * Q[:, None].float()).sum(-1) * D ** -0.5, 1)  # [N, L, H]
+        ref = (p[..., None] * v).sum(1)
+        nbytes = 2 * N * L * H * D * 2 + 2 * N * H * D * 2
+        return {"context": L, "attention_alone_us": round(ms * 1e3, 2), "attention_GBps": round(nbytes / ms / 1e6, 1),
+                "attention_bytes": nbytes, "attention_max_rel_err": float((O.float() - ref).abs().max() / ref.abs().max())}
+
+    return step, record
+
+
 def run_layer(args):
     """The four weight MatMuls of one OPT-30B-shaped decoder layer (hidden 7168, FFN 28672) back to back on one
-    stream, as eager calls and as one HIP graph, against the same four dense GEMMs.  One JSON line (not the bench
-    line).  The layers in a timed sequence rotate over copies of the weights (more than 1 GB in total)."""
+    stream, as eager calls and as one HIP graph, against the same four dense GEMMs and, with --layer-fp8, the same four
+    products in 8-bit floating point; with --layer-context L the attention over L keys stands between the first two in
+    all of them.  One JSON line (not the bench line).  The layers in a timed sequence rotate over copies of the weights
+    (more than 1 GB in total)."""
     import torch
 
     import fls_workloads as wl
@@ -479,6 +549,9 @@ def main():
                     help="instead of the bench line: the four MatMuls of one OPT-30B-shaped decoder layer back to back, "
                          "eager and as a HIP graph")
     ap.add_argument("--layer-n", type=int, default=16, help="with --layer: the batch size N")
+    ap.add_argument("--layer-context", type=int, default=0, metavar="L",
+                    help="with --layer: causal attention of every sequence over L keys between the QKV product and the output projection")
+    ap.add_argument("--layer-fp8", action="store_true", help="with --layer: the four products in 8-bit floating point as well")
     ap.add_argument("--entry", choices=("spmm", "noalloc"), default="spmm",
                     help="the entry point that is timed: fls_spmm, or fls_spmm_noalloc (N <= 32; it keeps to the narrow "
                          "kernel and clears its flags with a small kernel of its own before every call; the line is marked)")
@@ -496,6 +569,8 @@ def main():
         run_sweep(args)
         return
     if args.layer:
+        if args.layer_context < 0:
+            ap.error("--layer-context must not be negative")
         run_layer(args)
         return
     if args.crossover:
