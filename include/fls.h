@@ -14,6 +14,7 @@
  *   - C          : fp16, column-major M x N, leading dimension M   (== row-major [N][M])
  *   - products are exact, accumulation is fp32, C is rounded once to fp16 (nearest even)
  *   - M must be a multiple of FLS_TILE_M, K of FLS_TILE_K; 1 <= N <= FLS_MAX_N
+ *     (the 8-bit products and attention, below, say what they round and which shapes they take)
  *   - device pointers must be 16-byte aligned
  *   - kernels are enqueued on `stream` and the call returns without waiting, except
  *     fls_compress, which waits for its own work (it is an offline step, Sec. 5), the first
@@ -42,8 +43,8 @@ extern "C" {
 
 enum {
   FLS_OK = 0,
-  FLS_EINVAL = -1,     /* null pointer, M/K not multiples of the tile, N out of range, bad policy */
-  FLS_EALIGN = -2,     /* a device pointer is not 16-byte aligned */
+  FLS_EINVAL = -1,     /* null pointer, M/K not multiples of the tile, N out of range, bad policy, a shape not held */
+  FLS_EALIGN = -2,     /* a device pointer is not 16-byte aligned (arrays of 4-byte values of attention: 4-byte) */
   FLS_ECAPACITY = -3,  /* output buffer too small; stats->bytes_total holds the size needed */
   FLS_EFORMAT = -4,    /* blob header: bad magic / version / geometry, or M, K differ from the call */
   FLS_EWORKSPACE = -5, /* no workspace registered, or it is too small for this call */
@@ -148,7 +149,8 @@ size_t fls_workspace_bytes(int64_t M, int64_t K, int64_t N);
  * workspace must stay valid, and untouched by the caller, until replaced.  Nothing has to be
  * cleared between calls (every launch leaves the flags it raised lowered again), so one
  * registration serves any number of calls of any shape it is large enough for; calls that share
- * it must not overlap in time.  Errors: FLS_EINVAL, FLS_EALIGN, FLS_EHIP.
+ * it must not overlap in time.  A call that is recorded into a graph uses the workspace that was registered when it was
+ * recorded, in every replay.  Errors: FLS_EINVAL, FLS_EALIGN, FLS_EHIP.
  */
 int fls_set_workspace(void* ws_dev, size_t bytes, fls_stream_t stream);
 
@@ -297,8 +299,8 @@ typedef struct {
   int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head; /* strides: multiples of 8, rows of at most 2^22 */
   int32_t sequences, heads, kv_heads; /* kv_heads divides heads */
   int32_t head_dim;            /* a multiple of 8, at most FLS_MAX_HEAD_DIM */
-  int64_t max_q, max_k;        /* no sequence has more queries or keys; what one has beyond is not looked at */
-  float scale;                 /* positive and finite */
+  int64_t max_q, max_k;        /* no sequence has more queries or keys; one that does counts as cut to its first so many */
+  float scale;                 /* positive, at most 2e38 */
 } fls_attention_shape;
 
 #define FLS_MAX_HEAD_DIM 128
@@ -312,9 +314,14 @@ size_t fls_attention_workspace_bytes(const fls_attention_shape* shape_host);
  *   lse_dev    out: fp32 [heads][q_rows], natural logarithms; may be NULL
  *   shape_host  in: read during the call only
  * Uses the registered workspace; enqueues kernels only, so it may be recorded into a HIP graph and replayed with other lengths, as long as
- * max_q and max_k hold.  The lengths are read on the device: a sequence that lies outside 0 ... q_rows has no queries there, keys
- * outside 0 ... k_rows are left out.  Keys that a query does not see do not touch it, be they infinite or NaN.  O may not overlap Q, K or V.
- * The same call gives the same bits every time.  Errors: FLS_EINVAL, FLS_EALIGN, FLS_EWORKSPACE, FLS_EHIP.
+ * max_q and max_k hold.  The lengths are read on the device, and what lies outside the tensors is neither read nor written: a sequence whose
+ * queries are not all inside 0 ... q_rows has none, one whose k_start is outside 0 ... k_rows has no keys, one whose keys reach beyond k_rows has
+ * those up to there.  Keys that a query does not see do not touch it, be they infinite or NaN.  O may not overlap Q, K or V.
+ * The same call gives the same bits every time.  Nothing is launched, and no pointer looked at, where there is no query (sequences, q_rows or max_q is 0);
+ * K_dev and V_dev may be null where k_rows is 0.
+ * max_q decides how the work is cut: up to 64 queries (of all heads that share a key head) to a sequence, keys and values are read once for all
+ * of them; beyond, a workgroup takes 128 queries of a head.  Single tokens beside prompts of many are faster in a call of their own.
+ * Errors: FLS_EINVAL (also for work in more than 2^24 - 8 workgroups of 128 queries, or 2^29 of few), FLS_EALIGN, FLS_EWORKSPACE, FLS_EHIP.
  */
 int fls_attention(const void* Q_dev, const void* K_dev, const void* V_dev, void* O_dev, float* lse_dev, const int32_t* q_start_dev,
                   const int32_t* k_start_dev, const int32_t* k_len_dev, const fls_attention_shape* shape_host, fls_stream_t stream);

@@ -27,6 +27,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfls.so")
 _lib = None
 _ws_tensor = None  # keeps the registered workspace alive
+_ws_made = []      # and those that the ensure_... functions made: a recorded graph uses the one that was registered when it was recorded
 
 EXPORTS = ("fls_compress_bound", "fls_compress", "fls_compress_bound_v2", "fls_compress_v2", "fls_inspect", "fls_workspace_bytes", "fls_set_workspace",
            "fls_check_workspace", "fls_spmm", "fls_spmm_stats", "fls_spmm_noalloc", "fls_forget", "fls_dense_gemm", "fls_quantize",
@@ -181,7 +182,12 @@ def ensure_workspace(M, K, N):
     if need == 0:
         raise FlsError(EINVAL, "fls_workspace_bytes")
     if _ws_tensor is None or _ws_tensor.numel() < need:
-        fls_set_workspace(torch.empty(need, dtype=torch.uint8, device="cuda"))
+        _make_workspace(torch.empty(need, dtype=torch.uint8, device="cuda"))
+
+
+def _make_workspace(ws):
+    fls_set_workspace(ws)
+    _ws_made.append(ws)
 
 
 def fls_compress(W, out=None, order_policy=ORDER_LOCATION):
@@ -360,15 +366,15 @@ def fls_quantize(W, out=None):
     """W: float16 [M, K] CUDA tensor, K a multiple of 16.  Returns (Wq float8_e4m3fn [M, K], Ws float8_e8m0fnu [M, scale_stride(K)])."""
     import torch
 
-    assert W.is_cuda and W.dtype == torch.float16 and W.is_contiguous() and W.dim() == 2
+    assert _on_this_device(W) and W.dtype == torch.float16 and W.is_contiguous() and W.dim() == 2
     M, K = W.shape
     if out is None:
         Wq = torch.empty_like(W, dtype=torch.float8_e4m3fn)
         Ws = W.new_empty((M, scale_stride(K)), dtype=torch.float8_e8m0fnu)
     else:
         Wq, Ws = out
-        assert Wq.is_cuda and Wq.dtype == torch.float8_e4m3fn and Wq.is_contiguous() and Wq.shape == (M, K)
-        assert Ws.is_cuda and Ws.dtype == torch.float8_e8m0fnu and Ws.is_contiguous() and Ws.shape == (M, scale_stride(K))
+        assert _on_this_device(Wq, Ws) and Wq.dtype == torch.float8_e4m3fn and Wq.is_contiguous() and Wq.shape == (M, K)
+        assert Ws.dtype == torch.float8_e8m0fnu and Ws.is_contiguous() and Ws.shape == (M, scale_stride(K))
     rc = lib().fls_quantize(W.data_ptr(), M, K, Wq.data_ptr(), Ws.data_ptr(), _stream())
     if rc != OK:
         _check(rc, "fls_quantize")
@@ -385,11 +391,24 @@ def _ensure(need, where):
     if need == 0:
         raise FlsError(EINVAL, where)
     if _ws_tensor is None or _ws_tensor.numel() < need:
-        fls_set_workspace(torch.empty(need, dtype=torch.uint8, device="cuda"))
+        if torch.cuda.is_current_stream_capturing():  # memory of the graph's own, cleared in each replay
+            raise FlsError(EWORKSPACE, where)
+        # a power of two: all that were ever made are no more than twice the largest
+        _make_workspace(torch.empty(1 << (need - 1).bit_length(), dtype=torch.uint8, device="cuda"))
+
+
+def _on_this_device(*tensors):
+    import torch
+
+    device = tensors[0].get_device()  # -1: not on a GPU at all
+    for t in tensors[1:]:
+        if t.get_device() != device:
+            return False
+    return device >= 0 and device == torch.cuda.current_device()
 
 
 def ensure_fp8_workspace(M, K, N):
-    """ensure_workspace for fls_fp8_gemm."""
+    """ensure_workspace for fls_fp8_gemm; not while a graph is recorded, unless it is large enough already."""
     need = lib().fls_fp8_workspace_bytes(M, K, N)
     if need == 0 or _ws_tensor is None or _ws_tensor.numel() < need:
         _ensure(need, "fls_fp8_workspace_bytes")
@@ -398,10 +417,11 @@ def ensure_fp8_workspace(M, K, N):
 def _fp8_args(Wq, Ws, X, C, M, K, N):
     import torch
 
-    assert Wq.is_cuda and Wq.dtype == torch.float8_e4m3fn and Wq.is_contiguous() and Wq.shape == (M, K)
-    assert Ws.is_cuda and Ws.dtype == torch.float8_e8m0fnu and Ws.is_contiguous() and Ws.shape == (M, scale_stride(K))
-    assert X.is_cuda and X.dtype == torch.float16 and X.is_contiguous() and X.shape == (N, K)
-    assert C.is_cuda and C.dtype == torch.float16 and C.is_contiguous() and C.shape == (N, M)
+    assert _on_this_device(Wq, Ws, X, C)
+    assert Wq.dtype == torch.float8_e4m3fn and Wq.is_contiguous() and Wq.shape == (M, K)
+    assert Ws.dtype == torch.float8_e8m0fnu and Ws.is_contiguous() and Ws.shape == (M, scale_stride(K))
+    assert X.dtype == torch.float16 and X.is_contiguous() and X.shape == (N, K)
+    assert C.dtype == torch.float16 and C.is_contiguous() and C.shape == (N, M)
     return Wq.data_ptr(), Ws.data_ptr(), X.data_ptr(), C.data_ptr(), M, K, N, _stream()
 
 
@@ -440,7 +460,7 @@ def fls_attention_workspace_bytes(Q, K, sequences, max_q, max_k):
 
 
 def ensure_attention_workspace(Q, K, q_start, max_q, max_k):
-    """ensure_workspace for fls_attention."""
+    """ensure_workspace for fls_attention; not while a graph is recorded, unless it is large enough already."""
     need = _attention_workspace_bytes(*Q.shape, *K.shape[:2], q_start.shape[0] - 1, max_q, max_k)
     if need == 0 or _ws_tensor is None or _ws_tensor.numel() < need:
         _ensure(need, "fls_attention_workspace_bytes")
@@ -454,12 +474,12 @@ def _attention_args(Q, K, V, O, q_start, k_start, k_len, max_q, max_k, scale, ls
     k_rows, kv_heads, k_dim = k_shape = K.shape
     (q0, q1, q2), (k0, k1, k2), (v0, v1, v2), (o0, o1, o2) = Q.stride(), K.stride(), V.stride(), O.stride()
     sequences = k_len.shape[0]
-    assert Q.is_cuda and K.is_cuda and V.is_cuda and O.is_cuda and Q.dtype == f16 and K.dtype == f16 and V.dtype == f16 and O.dtype == f16
+    assert _on_this_device(Q, K, V, O, q_start, k_start, k_len) and Q.dtype == f16 and K.dtype == f16 and V.dtype == f16 and O.dtype == f16
     assert k_dim == dim and V.shape == k_shape and O.shape == shape and q2 == k2 == v2 == o2 == 1
-    assert q_start.is_cuda and k_start.is_cuda and k_len.is_cuda and q_start.dtype == i32 and k_start.dtype == i32 and k_len.dtype == i32
+    assert q_start.dtype == i32 and k_start.dtype == i32 and k_len.dtype == i32
     assert q_start.shape == (sequences + 1,) and k_start.shape == (sequences,) and q_start.is_contiguous() and k_start.is_contiguous() and k_len.is_contiguous()
     if lse is not None:
-        assert lse.is_cuda and lse.dtype == torch.float32 and lse.shape == (heads, q_rows) and lse.is_contiguous()
+        assert _on_this_device(lse) and lse.dtype == torch.float32 and lse.shape == (heads, q_rows) and lse.is_contiguous()
         lse = lse.data_ptr()
     if q_rows <= 1:  # the stride of one row or one head says nothing
         q0 = o0 = 0

@@ -611,14 +611,15 @@ int fls_fp8_gemm(const void* Wq_dev, const void* Ws_dev, const void* X_dev, void
   return fls::launch_fp8(a, (hipStream_t)stream) == hipSuccess ? FLS_OK : FLS_EHIP;
 }
 
-// What the attention kernels' arithmetic holds: rows and keys in 31 bits, a tile of 64 rows in a buffer descriptor, work in 2^29 units.
+// What the attention kernels' arithmetic holds: rows and keys in 31 bits, a tile of 64 rows in a buffer descriptor, scores in powers of two, work in 2^29
+// units; and what a row of a grid does: less than 2^32 threads, 256 to a workgroup (the kernel for many queries fills it up to a multiple of 8).
 static bool attention_shape_ok(const fls_attention_shape* s, fls::AttentionPlan* plan) {
   const int64_t rows = 0x7fffffffll, stride = (int64_t)1 << 22;
   if (s->q_rows < 0 || s->q_rows >= rows || s->k_rows < 0 || s->k_rows >= rows) return false;
   if (s->sequences < 0 || s->sequences > (1 << 24) || s->heads < 1 || s->heads > 65536 || s->kv_heads < 1 || s->heads % s->kv_heads != 0) return false;
   if (s->head_dim < 8 || s->head_dim > FLS_MAX_HEAD_DIM || s->head_dim % 8 != 0) return false;
   if (s->max_q < 0 || s->max_q >= rows || s->max_k < 0 || s->max_k >= rows - 4096) return false;
-  if (!(s->scale > 0.f) || s->scale > 3.4e38f) return false;
+  if (!(s->scale > 0.f) || s->scale > 2e38f) return false;
   const int64_t rowstr[4] = {s->q_row, s->k_row, s->v_row, s->o_row}, headstr[4] = {s->q_head, s->k_head, s->v_head, s->o_head};
   for (int i = 0; i < 4; ++i)
     if (rowstr[i] < 0 || rowstr[i] > stride || headstr[i] < 0 || headstr[i] > ((int64_t)1 << 40) || rowstr[i] % 8 != 0 || headstr[i] % 8 != 0) return false;
@@ -628,7 +629,7 @@ static bool attention_shape_ok(const fls_attention_shape* s, fls::AttentionPlan*
   if (!row_of_heads && !head_of_rows) return false;
   const int64_t max_q = s->max_q < s->q_rows ? s->max_q : s->q_rows, max_k = s->max_k < s->k_rows ? s->max_k : s->k_rows;
   *plan = fls::attention_plan(s->q_rows, (uint32_t)s->sequences, (uint32_t)s->heads, (uint32_t)s->kv_heads, (uint32_t)s->head_dim, max_q, max_k);
-  return plan->units < (1ull << 29) && (plan->chunks == 1 || plan->part_rows * s->heads < (1ull << 29));
+  return plan->units <= (plan->few ? (1ull << 29) - 1 : (1ull << 24) - 8) && (plan->chunks == 1 || plan->part_rows * s->heads < (1ull << 24));
 }
 
 size_t fls_attention_workspace_bytes(const fls_attention_shape* shape_host) {
@@ -640,8 +641,9 @@ size_t fls_attention_workspace_bytes(const fls_attention_shape* shape_host) {
 int fls_attention(const void* Q_dev, const void* K_dev, const void* V_dev, void* O_dev, float* lse_dev, const int32_t* q_start_dev,
                   const int32_t* k_start_dev, const int32_t* k_len_dev, const fls_attention_shape* shape_host, fls_stream_t stream) {
   fls::AttentionPlan plan;
-  if (!Q_dev || !K_dev || !V_dev || !O_dev || !q_start_dev || !k_start_dev || !k_len_dev || !shape_host || !attention_shape_ok(shape_host, &plan))
-    return FLS_EINVAL;
+  if (!shape_host || !attention_shape_ok(shape_host, &plan)) return FLS_EINVAL;
+  if (shape_host->sequences == 0 || shape_host->q_rows == 0 || shape_host->max_q == 0) return FLS_OK;  // no query
+  if (!Q_dev || !O_dev || !q_start_dev || !k_start_dev || !k_len_dev || (shape_host->k_rows != 0 && (!K_dev || !V_dev))) return FLS_EINVAL;
   if (!aligned16(Q_dev) || !aligned16(K_dev) || !aligned16(V_dev) || !aligned16(O_dev) || ((uintptr_t)lse_dev & 3u) != 0 ||
       (((uintptr_t)q_start_dev | (uintptr_t)k_start_dev | (uintptr_t)k_len_dev) & 3u) != 0)
     return FLS_EALIGN;
@@ -651,7 +653,6 @@ int fls_attention(const void* Q_dev, const void* K_dev, const void* V_dev, void*
     if (!g_ws || g_ws_bytes < kCounterAreaBytes + plan.parts_bytes) return FLS_EWORKSPACE;
     ws = (unsigned char*)g_ws;
   }
-  if (shape_host->sequences == 0 || shape_host->q_rows == 0 || shape_host->max_q == 0) return FLS_OK;  // no query
   const fls_attention_shape& s = *shape_host;
   fls::AttentionLaunch a;
   a.Q = (const _Float16*)Q_dev;

@@ -455,6 +455,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
 // up what they have at the end.
 
 constexpr uint32_t kFewKeys = 32;
+constexpr uint32_t kGridRow = 1u << 23;  // workgroups: a grid has less than 2^32 threads in a direction
 
 template <int DP, uint32_t WAVES>
 __global__ __launch_bounds__(WAVES * 64) void attention_few_kernel(AttentionParams p) {
@@ -464,7 +465,8 @@ __global__ __launch_bounds__(WAVES * 64) void attention_few_kernel(AttentionPara
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // chunk outermost: sequences of one length run side by side
   const uint32_t kv_heads = p.heads / p.rep;
-  uint32_t u = blockIdx.x;
+  const uint32_t u = blockIdx.y * gridDim.x + blockIdx.x;
+  if (u >= p.units) return;
   const uint32_t x = divide(u, p.by_row_blocks), block = u - x * p.row_blocks;
   const uint32_t y = divide(x, p.by_kv_heads), g = x - y * kv_heads;
   const uint32_t b = divide(y, p.by_chunks), c = y - b * p.chunks;
@@ -660,7 +662,7 @@ AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads,
 template <int DP>
 static hipError_t run(AttentionParams& p, const AttentionPlan& plan, hipStream_t stream) {
   if (plan.few && p.units <= 256u) attention_few_kernel<DP, 4><<<p.units, 256, 0, stream>>>(p);
-  else if (plan.few) attention_few_kernel<DP, 2><<<p.units, 128, 0, stream>>>(p);
+  else if (plan.few) attention_few_kernel<DP, 2><<<dim3(min(p.units, kGridRow), (p.units + kGridRow - 1u) / kGridRow), 128, 0, stream>>>(p);
   else attention_kernel<DP><<<(p.units + 7u) / 8u * 8u, 256, 0, stream>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.chunks == 1u) return e;

@@ -41,6 +41,7 @@ BAD = [dict(q_rows=-1), dict(k_rows=-1), dict(q_rows=(1 << 31) - 1), dict(k_rows
        dict(head_dim=0), dict(head_dim=65), dict(head_dim=136), dict(head_dim=-8), dict(max_q=-1), dict(max_k=-1), dict(max_q=1 << 31), dict(max_k=1 << 31), dict(scale=0.0), dict(scale=-1.0),
        dict(scale=float("inf")), dict(scale=float("nan")), dict(sequences=-1), dict(sequences=(1 << 24) + 1), dict(q_row=513), dict(k_row=-8),
        dict(v_row=(1 << 22) + 8), dict(k_head=(1 << 40) + 8), dict(v_head=4), dict(o_head=32), dict(o_row=448), dict(o_row=0), dict(o_head=0),
+       dict(scale=2.1e38), dict(sequences=1 << 24, heads=64, kv_heads=64, max_q=1, o_row=4096), dict(sequences=1 << 24, max_q=100),
        dict(q_rows=(1 << 31) - 2, heads=65536, kv_heads=65536, o_row=1 << 22, max_q=1 << 30)]
 
 
@@ -64,3 +65,24 @@ def test_pointers_refused(fls):
     # heads after one another, each a block of rows, is a layout as well; in places of one row or one head strides do not matter
     for ok in (dict(o_row=64, o_head=6400), dict(q_rows=1, o_row=0), dict(heads=1, kv_heads=1, o_head=0)):
         assert L.fls_attention_workspace_bytes(shape(fls, **ok)) > 0
+
+
+def test_nothing_to_do(fls):
+    """No query: nothing is launched and no pointer is looked at; no shape is let through for it."""
+    L = fls.lib()
+    for none in (dict(q_rows=0), dict(sequences=0), dict(max_q=0)):
+        assert L.fls_attention(*[None] * 8, shape(fls, **none), None) == fls.OK
+        assert L.fls_attention(*[None] * 8, shape(fls, head_dim=65, **none), None) == fls.EINVAL
+    for i in (0, 3, 5, 6, 7):  # K and V may be null where there are no keys, the others not
+        args = [16, None, None, 16, 16, 16, 16, 16, shape(fls, k_rows=0), None]
+        assert L.fls_attention(*[None if j == i else a for j, a in enumerate(args)]) == fls.EINVAL
+
+
+def test_the_binding_refuses_what_is_not_on_the_gpu(fls):
+    import torch
+
+    Q, n = torch.zeros(1, 1, 64, dtype=torch.float16), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(AssertionError):
+        fls.fls_attention(Q, Q, Q, Q, torch.zeros(2, dtype=torch.int32), n, n, 1, 1, 1.0)
+    with pytest.raises(AssertionError):
+        fls.fls_quantize(Q[0])

@@ -376,6 +376,114 @@ def test_a_layer_on_prompts_and_then_token_by_token(fls):
     assert (K.double() - cache_k[slabs[b]:slabs[b] + n].double()).norm() <= 2.0 ** -10 * K.double().norm()
 
 
+@pytest.mark.parametrize("H,G,D,nq,nk", [
+    (2, 1, 64, [n % 3 for n in range(200)], [5 * n % 71 + 2 for n in range(200)]),                                   # single tokens and pairs
+    (1, 1, 128, [70] + [n % 2 for n in range(150)] + [40], [75] + [7 * n % 400 + 1 for n in range(150)] + [3000]),   # 128 queries to a workgroup, chunks
+    (3, 3, 80, [130 if n % 40 == 7 else n % 2 for n in range(131)] + [300], [3 * n % 200 for n in range(131)] + [310]),
+], ids=["few", "chunks", "tiles"])
+def test_more_sequences_than_a_wave_has_lanes(fls, H, G, D, nq, nk):
+    import torch
+
+    Q, K, V, q_start, k_start, k_len = case(H, G, D, nq, nk, seed=len(nq), q_first=3, slack=1)
+    O, lse = attend(fls, Q, K, V, q_start, k_start, k_len, 0.2)
+    check(O, lse, reference(Q, K, V, q_start, k_start, k_len, 0.2))
+    # the same where max_q and max_k promise more than there is: other kernels, other chunks
+    for mq, mk in ((max(nq) * 100, max(nk)), (max(nq), 20000), (1 << 20, 1 << 28)):
+        P, lse = attend(fls, Q, K, V, q_start, k_start, k_len, 0.2, max_q=mq, max_k=mk)
+        check(P, lse, reference(Q, K, V, q_start, k_start, k_len, 0.2))
+
+
+def test_sequences_that_share_keys_and_are_cut(fls):
+    """Two sequences on the same keys (a shared prefix); and max_q, max_k below what a sequence has: its first so many of each."""
+    Q, K, V, q_start, _, _ = case(4, 2, 64, [3, 2, 140], [400], seed=13)
+    for mq, mk in ((140, 300), (140, 100), (64, 300), (2, 33)):
+        k_start, k_len = [3, 3, 20], [300, 200, 250]
+        O, lse = attend(fls, Q, K, V, q_start, k_start, k_len, 0.2, max_q=mq, max_k=mk)
+        for b in range(3):
+            n, cut = min(q_start[b + 1] - q_start[b], mq), min(k_len[b], mk)
+            rows = slice(q_start[b], q_start[b] + n)
+            check(O[rows], lse[:, rows].contiguous(), reference(Q[rows], K, V, [0, n], [k_start[b]], [cut], 0.2))
+            assert (O[q_start[b] + n:q_start[b + 1]] == 5).all()
+
+
+def test_nothing_to_attend(fls):
+    import torch
+
+    e = lambda *s: torch.empty(s, dtype=torch.float16, device="cuda")  # noqa: E731
+    O = torch.full((3, 2, 64), 5.0, dtype=torch.float16, device="cuda")
+    fls.ensure_attention_workspace(O, e(0, 1, 64), ints([0, 3]), 3, 0)
+    assert fls.fls_attention(e(0, 2, 64), e(0, 1, 64), e(0, 1, 64), e(0, 2, 64), ints([0, 0]), ints([0]), ints([0]), 0, 0, 1.0).shape == (0, 2, 64)
+    assert (fls.fls_attention(e(3, 2, 64), e(7, 1, 64), e(7, 1, 64), O, ints([0]), ints([]), ints([]), 3, 7, 1.0) == 5).all()  # no sequence
+    for max_k in (0, 9):  # no key
+        lse = torch.zeros(2, 3, device="cuda")
+        O.fill_(5.0)
+        fls.fls_attention(e(3, 2, 64), e(0, 1, 64), e(0, 1, 64), O, ints([0, 3]), ints([0]), ints([0]), 3, max_k, 1.0, lse)
+        assert (O == 0).all() and (lse == -math.inf).all()
+
+
+def test_very_many_sequences(fls):
+    """More workgroups than a grid has in one direction: single tokens with one key each, whose values are the result."""
+    import torch
+
+    n, H, D = 300000, 32, 8
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    Q = torch.randn(n, H, D, generator=gen, device="cuda").half()
+    V = torch.randn(1000, H, D, generator=gen, device="cuda").half()
+    k_start = torch.randint(0, 1000, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    q_start, k_len = torch.arange(n + 1, device="cuda", dtype=torch.int32), torch.ones(n, device="cuda", dtype=torch.int32)
+    O = torch.zeros_like(Q)
+    fls.ensure_attention_workspace(Q, V, q_start, 1, 1)
+    fls.fls_attention(Q, V, V, O, q_start, k_start, k_len, 1, 1, 1.0)
+    assert torch.equal(O, V[k_start.long()])
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_drawn(fls, seed):
+    """Shapes and lengths drawn over what the call takes."""
+    import random
+
+    r = random.Random(seed)
+    G = r.choice((1, 1, 2, 3, 5))
+    H, D = G * r.choice((1, 1, 2, 3, 4, 7, 8, 13)), 8 * r.randint(1, 16)
+    longest = r.choice((1, 1, 2, 5, 16, 64, 200, 700))
+    nq = [r.randint(0, longest) if r.random() < 0.8 else longest for _ in range(r.choice((1, 1, 2, 3, 7, 12)))]
+    nk = [max(0, n + r.choice((0, 0, 1, 63, 64, 300, 5000, -1, -n // 2))) for n in nq]
+    Q, K, V, q_start, k_start, k_len = case(H, G, D, nq, nk, seed=seed, q_first=r.choice((0, 1)), slack=r.choice((0, 3)), spread=r.choice((0.1, 1.0, 4.0)))
+    scale = r.choice((1.0, D ** -0.5, 0.01))
+    O, lse = attend(fls, Q, K, V, q_start, k_start, k_len, scale)
+    check(O, lse, reference(Q, K, V, q_start, k_start, k_len, scale))
+
+
+def test_a_graph_keeps_its_workspace(fls):
+    """A call that was recorded before a larger workspace was made writes its partial sums where it did."""
+    import torch
+
+    Q, K, V, q_start, k_start, k_len = case(2, 1, 64, [1, 1], [9000, 8000], seed=17)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        qs, ks, kl = ints(q_start), ints(k_start), ints(k_len)
+        fls._ws_tensor = None  # as in a new process
+        fls.ensure_attention_workspace(Q, K, qs, 1, 9000)
+        O, P = torch.zeros_like(Q), torch.zeros_like(Q)
+        fls.fls_attention(Q, K, V, O, qs, ks, kl, 1, 9000, 0.1)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            fls.fls_attention(Q, K, V, P, qs, ks, kl, 1, 9000, 0.1)
+            with pytest.raises(fls.FlsError) as e:  # a larger one cannot be made here
+                fls.ensure_fp8_workspace(128, 1 << 17, 64)
+            assert e.value.code == fls.EWORKSPACE
+        size = fls._ws_tensor.numel()
+        fls.ensure_fp8_workspace(128, 1 << 17, 64)
+        assert fls._ws_tensor.numel() > size
+        others = [torch.full((size,), 0x7f, dtype=torch.uint8, device="cuda") for _ in range(3)]
+        for i in range(3):
+            P.zero_()
+            graph.replay()
+            side.synchronize()
+            assert torch.equal(O, P) and all((t == 0x7f).all() for t in others)
+
+
 def test_refusals_in_the_binding(fls):
     import torch
 

@@ -214,6 +214,52 @@ def test_same_bits_each_time_and_in_a_graph(fls, M, K, N):
             assert torch.equal(C, D) and C.abs().max() > 0
 
 
+def test_a_matrix_past_32_bits(fls):
+    """Elements and bytes of W past 2^32: its last rows against the same rows alone."""
+    import torch
+
+    M, K = (1 << 20) + 77, 4112
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    W = torch.empty(M, K, dtype=torch.float16, device="cuda")
+    rows = [0, 1, 522247, 522248, 1044495, 1044496] + list(range(M - 130, M))  # the rows in which 2^32 bytes of fp16 and of e4m3 are full
+    W.fill_(0.5)
+    W[rows] = torch.randn(len(rows), K, generator=gen, device="cuda").half()
+    Wq, Ws = fls.fls_quantize(W)
+    part = W[rows]
+    del W
+    q, s = fls.fls_quantize(part)
+    assert torch.equal(Wq.view(torch.uint8)[rows], q.view(torch.uint8)) and torch.equal(Ws.view(torch.uint8)[rows], s.view(torch.uint8))
+    plain = q.double() * torch.exp2(s.view(torch.uint8).double() - 127).repeat_interleave(128, 1)[:, :K]
+    for N in (3, 40, 100):
+        X = torch.randint(-2, 3, (N, K), generator=gen, device="cuda").half()  # exact in e4m3
+        fls.ensure_fp8_workspace(M, K, N)
+        C = torch.empty(N, M, dtype=torch.float16, device="cuda")
+        fls.fls_fp8_gemm(Wq, Ws, X, C, M, K, N)
+        ref, size = X.double() @ plain.T, X.double().abs() @ plain.abs().T
+        got = C[:, rows].double()
+        assert ((got - ref).abs() <= 2.0 ** -11 * ref.abs() + 2.0 ** -13 * size + 2.0 ** -25).all()
+        half = X.double().sum(1) * 0.5
+        assert ((C[:, 2000:3000].double() - half[:, None]).abs() <= (2.0 ** -11 * half.abs() + 2.0 ** -13 * X.double().abs().sum(1) * 0.5)[:, None]).all()
+
+
+def test_refusals_in_the_binding(fls):
+    import torch
+
+    W = torch.zeros(8, 32, dtype=torch.float16, device="cuda")
+    X, C = torch.zeros(3, 32, dtype=torch.float16, device="cuda"), torch.zeros(3, 8, dtype=torch.float16, device="cuda")
+    for bad in (W.float(), W.cpu(), W.T, W[0]):
+        with pytest.raises(AssertionError):
+            fls.fls_quantize(bad)
+    with pytest.raises(fls.FlsError) as e:
+        fls.fls_quantize(W[:, :24].contiguous())
+    assert e.value.code == fls.EINVAL
+    Wq, Ws = fls.fls_quantize(W)
+    fls.ensure_fp8_workspace(8, 32, 3)
+    for bad in ((W, Ws, X, C), (Wq, Ws.view(torch.uint8), X, C), (Wq, Ws[:, :3], X, C), (Wq, Ws, X.float(), C), (Wq, Ws, X[:2], C), (Wq, Ws, X, C.T), (Wq, Ws, X.cpu(), C)):
+        with pytest.raises(AssertionError):
+            fls.fls_fp8_gemm(*bad, 8, 32, 3)
+
+
 def test_next_to_the_dense_and_the_sparse_product(fls):
     """One workspace serves all products of a layer in turn."""
     import torch
