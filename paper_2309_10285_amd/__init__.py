@@ -125,13 +125,16 @@ def strerror(code):
 
 
 _raw_stream = None
+_several_devices = False
 
 
 def _stream():
     """The current stream of the current device, as hipStream_t."""
-    global _raw_stream
+    global _raw_stream, _several_devices
     if _raw_stream is None:
         import torch
+
+        _several_devices = torch.cuda.device_count() > 1
 
         torch.cuda.current_stream()  # initialises torch's GPU side, or raises
         # what that call is made of, without the Stream object: a microsecond less, but names that torch does not promise
@@ -366,16 +369,18 @@ def fls_quantize(W, out=None):
     """W: float16 [M, K] CUDA tensor, K a multiple of 16.  Returns (Wq float8_e4m3fn [M, K], Ws float8_e8m0fnu [M, scale_stride(K)])."""
     import torch
 
-    assert _on_this_device(W) and W.dtype == torch.float16 and W.is_contiguous() and W.dim() == 2
+    assert W.is_cuda and W.dtype == torch.float16 and W.is_contiguous() and W.dim() == 2
     M, K = W.shape
     if out is None:
         Wq = torch.empty_like(W, dtype=torch.float8_e4m3fn)
         Ws = W.new_empty((M, scale_stride(K)), dtype=torch.float8_e8m0fnu)
     else:
         Wq, Ws = out
-        assert _on_this_device(Wq, Ws) and Wq.dtype == torch.float8_e4m3fn and Wq.is_contiguous() and Wq.shape == (M, K)
-        assert Ws.dtype == torch.float8_e8m0fnu and Ws.is_contiguous() and Ws.shape == (M, scale_stride(K))
-    rc = lib().fls_quantize(W.data_ptr(), M, K, Wq.data_ptr(), Ws.data_ptr(), _stream())
+        assert Wq.is_cuda and Wq.dtype == torch.float8_e4m3fn and Wq.is_contiguous() and Wq.shape == (M, K)
+        assert Ws.is_cuda and Ws.dtype == torch.float8_e8m0fnu and Ws.is_contiguous() and Ws.shape == (M, scale_stride(K))
+    stream = _stream()
+    assert not _several_devices or _on_this_device(W, Wq, Ws)
+    rc = lib().fls_quantize(W.data_ptr(), M, K, Wq.data_ptr(), Ws.data_ptr(), stream)
     if rc != OK:
         _check(rc, "fls_quantize")
     return Wq, Ws
@@ -398,13 +403,11 @@ def _ensure(need, where):
 
 
 def _on_this_device(*tensors):
+    """Called where there are several devices: that of the stream has to be the tensors'."""
     import torch
 
-    device = tensors[0].get_device()  # -1: not on a GPU at all
-    for t in tensors[1:]:
-        if t.get_device() != device:
-            return False
-    return device >= 0 and device == torch.cuda.current_device()
+    device = torch.cuda.current_device()
+    return all(t.get_device() == device for t in tensors)
 
 
 def ensure_fp8_workspace(M, K, N):
@@ -417,12 +420,13 @@ def ensure_fp8_workspace(M, K, N):
 def _fp8_args(Wq, Ws, X, C, M, K, N):
     import torch
 
-    assert _on_this_device(Wq, Ws, X, C)
-    assert Wq.dtype == torch.float8_e4m3fn and Wq.is_contiguous() and Wq.shape == (M, K)
-    assert Ws.dtype == torch.float8_e8m0fnu and Ws.is_contiguous() and Ws.shape == (M, scale_stride(K))
-    assert X.dtype == torch.float16 and X.is_contiguous() and X.shape == (N, K)
-    assert C.dtype == torch.float16 and C.is_contiguous() and C.shape == (N, M)
-    return Wq.data_ptr(), Ws.data_ptr(), X.data_ptr(), C.data_ptr(), M, K, N, _stream()
+    assert Wq.is_cuda and Wq.dtype == torch.float8_e4m3fn and Wq.is_contiguous() and Wq.shape == (M, K)
+    assert Ws.is_cuda and Ws.dtype == torch.float8_e8m0fnu and Ws.is_contiguous() and Ws.shape == (M, scale_stride(K))
+    assert X.is_cuda and X.dtype == torch.float16 and X.is_contiguous() and X.shape == (N, K)
+    assert C.is_cuda and C.dtype == torch.float16 and C.is_contiguous() and C.shape == (N, M)
+    stream = _stream()
+    assert not _several_devices or _on_this_device(Wq, Ws, X, C)
+    return Wq.data_ptr(), Ws.data_ptr(), X.data_ptr(), C.data_ptr(), M, K, N, stream
 
 
 def fls_fp8_gemm(Wq, Ws, X, C, M, K, N):
@@ -474,13 +478,14 @@ def _attention_args(Q, K, V, O, q_start, k_start, k_len, max_q, max_k, scale, ls
     k_rows, kv_heads, k_dim = k_shape = K.shape
     (q0, q1, q2), (k0, k1, k2), (v0, v1, v2), (o0, o1, o2) = Q.stride(), K.stride(), V.stride(), O.stride()
     sequences = k_len.shape[0]
-    assert _on_this_device(Q, K, V, O, q_start, k_start, k_len) and Q.dtype == f16 and K.dtype == f16 and V.dtype == f16 and O.dtype == f16
+    assert Q.is_cuda and K.is_cuda and V.is_cuda and O.is_cuda and Q.dtype == f16 and K.dtype == f16 and V.dtype == f16 and O.dtype == f16
     assert k_dim == dim and V.shape == k_shape and O.shape == shape and q2 == k2 == v2 == o2 == 1
-    assert q_start.dtype == i32 and k_start.dtype == i32 and k_len.dtype == i32
-    assert q_start.shape == (sequences + 1,) and k_start.shape == (sequences,) and q_start.is_contiguous() and k_start.is_contiguous() and k_len.is_contiguous()
+    assert q_start.is_cuda and k_start.is_cuda and k_len.is_cuda and q_start.dtype == i32 and k_start.dtype == i32 and k_len.dtype == i32
+    assert q_start.shape == (sequences + 1,) and k_start.shape == k_len.shape == (sequences,) and q_start.is_contiguous() and k_start.is_contiguous() and k_len.is_contiguous()
     if lse is not None:
-        assert _on_this_device(lse) and lse.dtype == torch.float32 and lse.shape == (heads, q_rows) and lse.is_contiguous()
-        lse = lse.data_ptr()
+        assert lse.is_cuda and lse.dtype == torch.float32 and lse.shape == (heads, q_rows) and lse.is_contiguous()
+    stream = _stream()
+    assert not _several_devices or _on_this_device(Q, K, V, O, q_start, k_start, k_len, Q if lse is None else lse)
     if q_rows <= 1:  # the stride of one row or one head says nothing
         q0 = o0 = 0
     if k_rows <= 1:
@@ -489,8 +494,8 @@ def _attention_args(Q, K, V, O, q_start, k_start, k_len, max_q, max_k, scale, ls
         q1 = o1 = 0
     if kv_heads == 1:
         k1 = v1 = 0
-    return (Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), lse, q_start.data_ptr(), k_start.data_ptr(), k_len.data_ptr(),
-            _pack_attention(q_rows, k_rows, q0, q1, k0, k1, v0, v1, o0, o1, sequences, heads, kv_heads, dim, max_q, max_k, scale), _stream())
+    return (Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), None if lse is None else lse.data_ptr(), q_start.data_ptr(), k_start.data_ptr(), k_len.data_ptr(),
+            _pack_attention(q_rows, k_rows, q0, q1, k0, k1, v0, v1, o0, o1, sequences, heads, kv_heads, dim, max_q, max_k, scale), stream)
 
 
 def fls_attention(Q, K, V, O, q_start, k_start, k_len, max_q, max_k, scale, lse=None):

@@ -41,7 +41,7 @@ struct AttentionParams {
   float* part_ml;             // [chunk][part row][head][2]
   uint64_t part_rows;
   uint32_t few;
-  Divisor by_rep, by_chunks, by_row_blocks, by_kv_heads, by_slots, by_heads, by_max_q;
+  Divisor by_rep, by_chunks, by_chunk, by_row_blocks, by_kv_heads, by_slots, by_heads, by_max_q;
 };
 
 // A sequence, cut to the tensors it lies in: whatever the arrays hold, nothing outside is read or written.
@@ -59,6 +59,9 @@ __device__ __forceinline__ Sequence sequence(const AttentionParams& p, uint32_t 
   s.nk = min(s.nk, p.max_k);
   return s;
 }
+
+// Chunks that so many keys are cut into.  One chunk goes to O at once.
+__device__ __forceinline__ uint32_t chunks_of(uint32_t keys, const AttentionParams& p) { return keys <= p.chunk ? 1u : divide((keys - 1u) >> 7, p.by_chunk) + 1u; }
 
 // Head sizes are filled up to DP = 64, 96 or 128 with zeros; a row in LDS has 64 or 128 values.
 template <int DP>
@@ -314,9 +317,9 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t unit;
   if (!xcd_unit(p.units, unit)) return;
-  // head by head, so that what runs at one time on an XCD reads the same keys
-  const uint32_t whole = divide(unit, p.by_chunks), c = unit - whole * p.chunks;
-  const uint32_t head = divide(whole, p.by_slots), slot = whole - head * p.slots;
+  // head by head and chunk by chunk, so that what runs at one time on an XCD reads the same keys
+  const uint32_t whole = divide(unit, p.by_slots), slot = unit - whole * p.slots;
+  const uint32_t head = divide(whole, p.by_chunks), c = whole - head * p.chunks;
   // Slots are counted over the sequences, one for each 128 queries; those left over lie at the end of a head.  (Slots that can be told from
   // q_start alone, with one to spare for each sequence, left every second one empty for sequences of 128: the CUs that the hardware gives those to had half the
   // work, and 64 such sequences took twice as long.)  A lane looks at one sequence; what is known of the one that has the slot comes from its lane.
@@ -356,13 +359,9 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
   const int last = (int)min(first + kTileQ, s.nq) - 1 + off;  // last key that the workgroup's last query sees,
   const int low = (int)first + off;                           // its first query,
   const int wave_low = low + (int)wave * 32, high = min(wave_low + 31, (int)s.nk - 1);  // the wave's first and last
-  const uint32_t keys = last < 0 ? 0u : (uint32_t)last + 1u;
-  uint32_t t0 = 0, t1 = (keys + kTileKeys - 1) / kTileKeys;
-  if (p.chunks > 1u) {
-    if (c * (uint64_t)p.chunk >= s.nk) return;  // no such chunk
-    t0 = c * (p.chunk / kTileKeys);
-    t1 = min(t1, t0 + p.chunk / kTileKeys);
-  }
+  const uint32_t keys = last < 0 ? 0u : (uint32_t)last + 1u, parts = chunks_of(keys, p);
+  if (c >= parts) return;  // no such chunk
+  const uint32_t t0 = c * (p.chunk / kTileKeys), t1 = min((keys + kTileKeys - 1u) / kTileKeys, t0 + p.chunk / kTileKeys);
   const uint32_t full = low < 0 ? 0u : ((uint32_t)low + 1u) / kTileKeys;  // tiles that all see (the same for all waves)
   auto issue = [&](uint32_t t, uint32_t to) {
     const int64_t row = s.k0 + (int64_t)t * kTileKeys;
@@ -414,7 +413,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
   }
   w.l = across(w.l, true);
   const int64_t row = s.q0 + mine;
-  if (p.chunks == 1u) {
+  if (parts == 1u) {
     // Through LDS, so that 16 (8) lanes write a row: stores of the 8 bytes that a lane has of its query took a seventh of short prompts' time.
     __syncthreads();  // nobody reads a tile any more
     constexpr uint32_t kRow = kPitch<DP> * 2, kPieces = kPitch<DP> / 8;
@@ -473,9 +472,9 @@ __global__ __launch_bounds__(WAVES * 64) void attention_few_kernel(AttentionPara
   const Sequence s = sequence(p, b);
   const uint32_t rows = s.nq * p.rep;
   if (block * 32u >= rows) return;
-  const uint32_t begin = p.chunks > 1u ? c * p.chunk : 0u;
-  if (p.chunks > 1u && begin >= s.nk) return;  // no such chunk
-  const uint32_t end = p.chunks > 1u ? min(s.nk, begin + p.chunk) : s.nk;
+  const uint32_t parts = chunks_of(s.nk, p), begin = c * p.chunk;
+  if (c >= parts) return;  // no such chunk
+  const uint32_t end = min(s.nk, begin + p.chunk);
   const int off = (int)s.nk - (int)s.nq;
 
   Wave<DP> w;
@@ -559,7 +558,7 @@ __global__ __launch_bounds__(WAVES * 64) void attention_few_kernel(AttentionPara
       }
     }
   const int64_t row = s.q0 + query;
-  if (p.chunks == 1u) {
+  if (parts == 1u) {
     store_rows<DP>(w, p.O + row * p.o_row + (int64_t)head * p.o_head, l > 0.f ? 1.f / l : l, p.dim, lane);
     if (p.lse && lane < 32u) p.lse[(int64_t)head * p.q_rows + row] = log_sum(m, l);
     return;
@@ -579,36 +578,41 @@ __global__ __launch_bounds__(WAVES * 64) void attention_few_kernel(AttentionPara
 
 // --- chunks joined --------------------------------------------------------------------------------------------------------------
 // 32 lanes have four d each of a query row and head, LANES of them side by side every LANES-th chunk; a block has 8 / LANES rows and heads.  The largest m
-// of all chunks comes first, so that no load waits for another one's result.  Sums are added in a fixed order.
+// of all chunks comes first, so that no load waits for another one's result.  Sums are added in a fixed order.  What has only one chunk of keys that it sees is in
+// O already.  (Sums for all of it, and 8 lanes side by side for any number of rows: 64 heads, 2048 queries in three chunks, 307 us instead of 134.)
 template <int DP, int LANES>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p) {
   __shared__ float4v sum_o[8][32];
   __shared__ float sum_l[8];
   const uint32_t lane = threadIdx.x & 63u, part = threadIdx.x >> 5, mine = part % LANES;
-  const uint32_t pair = blockIdx.x * (8u / LANES) + part / LANES;  // the same for a wave
+  const uint32_t pair = blockIdx.x * (8u / LANES) + part / LANES;
   const uint32_t part_row = divide(pair, p.by_heads), head = pair - part_row * p.heads, d = (threadIdx.x & 31u) * 4u;
   uint32_t b = 0;
   if (p.few) {
     b = divide(part_row, p.by_max_q) + 1u;
   } else {
-    for (uint32_t at = 0; at < p.sequences; at += 64u) {
-      const uint32_t i = at + lane;
-      b += __popcll(__ballot(i < p.sequences && p.q_start[min(i, p.sequences - 1u)] <= (int64_t)part_row));
+    for (uint32_t at = 0; at < p.sequences; at += 32u) {  // half a wave has one row
+      const uint32_t i = at + (lane & 31u);
+      const uint64_t begun = __ballot(i < p.sequences && p.q_start[min(i, p.sequences - 1u)] <= (int64_t)part_row);
+      b += __popc((uint32_t)(begun >> (lane & 32u)));
     }
   }
   Sequence s = {0, 0, 0u, 0u};
   if (b > 0u && part_row < p.part_rows) s = sequence(p, b - 1u);
   const int64_t row = p.few ? s.q0 + (part_row - (b - 1u) * p.max_q) : (int64_t)part_row;
-  const bool there = row >= s.q0 && row < s.q0 + s.nq;
-  const uint32_t n = there ? min((s.nk + p.chunk - 1u) / p.chunk, p.chunks) : 0u;
+  // where there is one chunk, it is in O already
+  uint32_t keys = s.nk;
+  if (!p.few) keys = (uint32_t)max(0, (int)min(((uint32_t)(row - s.q0) | (kTileQ - 1u)) + 1u, s.nq) + (int)s.nk - (int)s.nq);  // of the row's workgroup
+  const uint32_t n = chunks_of(keys, p);
+  const bool there = row >= s.q0 && row < s.q0 + s.nq && n > 1u;
   const uint64_t first = (uint64_t)part_row * p.heads + head, step = p.part_rows * p.heads;
   float m = -kInf;
 #pragma unroll 4
-  for (uint32_t c = 0; c < n; ++c) m = fmaxf(m, p.part_ml[(first + c * step) * 2]);
+  for (uint32_t c = 0; c < (there ? n : 0u); ++c) m = fmaxf(m, p.part_ml[(first + c * step) * 2]);
   float l = 0.f;
   float4v o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (uint32_t c = mine; c < n; c += LANES) {
+  for (uint32_t c = mine; c < (there ? n : 0u); c += LANES) {
     const float mc = p.part_ml[(first + c * step) * 2], lc = p.part_ml[(first + c * step) * 2 + 1];
     const float4v oc = d < (uint32_t)DP ? *(const float4v*)(p.part_o + (first + c * step) * DP + d) : float4v{0.f, 0.f, 0.f, 0.f};
     const float down = mc == -kInf ? 0.f : __builtin_amdgcn_exp2f(mc - m);  // a chunk of which the query sees no key: its l and o are 0 (or NaN, which stays)
@@ -638,6 +642,25 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p) 
 
 static uint32_t padded_dim(uint32_t dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : 128; }
 
+// Chunks for many queries, by an estimate (us) that takes all sequences to have max_k keys.  `busy` workgroups of 128 queries, two to a CU: a tile of 64 keys takes
+// 1.15 us where half of the CUs have one, 1.6 one on each, 2.2 two on each (of 96 values 0.86 of that, of 64 0.73); sums are written and read, and a second kernel is
+// started.  512 queries, 64 heads of 128, in front of 512, 2512 and 8512 keys, one chunk and two: 21 and 29, 72 and 66, 216 and 163 us; 32 heads and 8512 keys
+// in one, two, four and eight: 153, 129, 91, 105.
+static uint32_t chunks_of_many(uint64_t busy, uint64_t part_rows_heads, uint32_t DP, uint64_t max_k, uint64_t most) {
+  uint32_t best = 1;
+  float least = 3e38f;
+  for (uint32_t c = 1; c == 1 || (c <= most && c * busy <= 1024); c += 1 + c / 8) {
+    const float units = (float)(c * busy), tiles = (float)((max_k + 64 * c - 1) / (64 * c));
+    const float tile = (0.45f + 0.0043f * DP) * (units <= 128.f ? 1.15f : units <= 256.f ? 1.15f + (units - 128.f) * 0.0036f : units <= 512.f ? 1.6f + (units - 256.f) * 0.0023f : units * 0.0043f);
+    const float us = tiles * tile + (c == 1 ? 0.f : 3.f + (float)part_rows_heads * c * DP * (8.f / 4.5e6f));
+    if (us < least) {
+      least = us;
+      best = c;
+    }
+  }
+  return best;
+}
+
 AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads, uint32_t kv_heads, uint32_t dim, int64_t max_q, int64_t max_k) {
   AttentionPlan plan = {};
   const uint64_t packed = (uint64_t)max_q * (heads / kv_heads);  // rows of queries that share keys
@@ -645,7 +668,7 @@ AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads,
   plan.row_blocks = (uint32_t)((packed + 31) / 32);
   // workgroups with work if the keys are not split: about
   const uint64_t busy = plan.few ? (uint64_t)sequences * kv_heads * plan.row_blocks : ((uint64_t)q_rows + kTileQ - 1) / kTileQ * heads;
-  const uint64_t wanted = (plan.few ? 512u : 256u) / (busy ? busy : 1), most = ((uint64_t)max_k + 255) / 256;
+  const uint64_t most = ((uint64_t)max_k + 255) / 256, wanted = plan.few ? 512u / (busy ? busy : 1) : chunks_of_many(busy, q_rows * heads, padded_dim(dim), max_k, most);
   uint64_t chunks = wanted < most ? wanted : most;
   if (chunks < 1) chunks = 1;
   plan.chunk = (uint32_t)((((uint64_t)max_k + chunks - 1) / chunks + 127) / 128 * 128);
@@ -667,7 +690,8 @@ static hipError_t run(AttentionParams& p, const AttentionPlan& plan, hipStream_t
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.chunks == 1u) return e;
   const uint64_t pairs = p.part_rows * p.heads;
-  if (p.chunks <= 2u) attention_join_kernel<DP, 2><<<(uint32_t)((pairs + 3u) / 4u), 256, 0, stream>>>(p);
+  if (pairs >= 8192u) attention_join_kernel<DP, 1><<<(uint32_t)((pairs + 7u) / 8u), 256, 0, stream>>>(p);
+  else if (p.chunks <= 2u) attention_join_kernel<DP, 2><<<(uint32_t)((pairs + 3u) / 4u), 256, 0, stream>>>(p);
   else attention_join_kernel<DP, 8><<<(uint32_t)pairs, 256, 0, stream>>>(p);
   return hipGetLastError();
 }
@@ -687,6 +711,7 @@ hipError_t launch_attention(const AttentionLaunch& a, const AttentionPlan& plan,
   p.part_rows = plan.part_rows;
   p.few = plan.few;
   p.by_heads = divisor(a.heads), p.by_max_q = divisor((uint32_t)a.max_q);
+  p.by_chunk = divisor(p.chunk / 128u);
   p.by_rep = divisor(p.rep), p.by_chunks = divisor(p.chunks), p.by_kv_heads = divisor(a.kv_heads);
   p.row_blocks = plan.row_blocks, p.slots = plan.slots, p.units = (uint32_t)plan.units;
   p.by_row_blocks = divisor(plan.few ? p.row_blocks : 1u), p.by_slots = divisor(p.slots);

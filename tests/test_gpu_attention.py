@@ -497,3 +497,22 @@ def test_refusals_in_the_binding(fls):
         with pytest.raises(fls.FlsError) as e:
             fls.fls_attention(*args(**bad))
         assert e.value.code == fls.EINVAL
+
+
+def test_tensors_of_another_device_are_refused(fls, monkeypatch):
+    """As on a machine with two of them, of which the other one is the current one."""
+    import torch
+
+    Q, K, V, q_start, k_start, k_len = case(2, 1, 64, [2], [5])
+    call = lambda: fls.fls_attention(Q, K, V, torch.empty_like(Q), ints(q_start), ints(k_start), ints(k_len), 2, 5, 1.0)  # noqa: E731
+    W = torch.zeros(8, 128, dtype=torch.float16, device="cuda")
+    Wq, Ws = fls.fls_quantize(W)
+    fls.ensure_fp8_workspace(8, 128, 8)
+    product = lambda: fls.fls_fp8_gemm(Wq, Ws, W, torch.empty(8, 8, dtype=torch.float16, device="cuda"), 8, 128, 8)  # noqa: E731
+    monkeypatch.setattr(fls, "_several_devices", True)
+    for f in (call, product, lambda: fls.fls_quantize(W)):
+        f()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for f in (call, product, lambda: fls.fls_quantize(W)):
+        with pytest.raises(AssertionError):
+            f()
