@@ -61,7 +61,8 @@ __device__ __forceinline__ u32x4 to_e4m3(const u32x4& a, const u32x4& b, uint32_
 }
 
 // Rows of fp16 -> e4m3 [rows][K] and scales [rows][stride].  Bound by memory: 2 bytes in, 1 out.  A lane takes 16 values (32 B in,
-// 16 B out), the eight lanes of a block agree on its largest.  Blocks from K on, up to the stride, have a scale of one.
+// 16 B out), the eight lanes of a block agree on its largest.  Blocks from K on, up to the stride, have a scale of one.  Loads that the caches need not keep and
+// ordinary stores: 28672 x 7168 96 us, 6.4 TB/s; both ordinary 106, neither kept 102.
 // FRAGMENTS: the values as the stream kernel reads them, [step][16 rows][half][lane][16] with `columns` groups of 16 rows, whole steps.
 template <bool FRAGMENTS>
 __global__ __launch_bounds__(256) void quantize_kernel(const _Float16* W, uint8_t* q, uint8_t* s, uint32_t K, uint32_t stride, Divisor by_slots, uint64_t rows, uint32_t columns) {
@@ -92,7 +93,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(const _Float16* W, uint8_
     if (here && step * kBlock < K)
       *(u32x4*)(q + (((uint64_t)step * columns + row / 16u) * 2u + piece % 2u) * 1024u + (piece / 2u * 16u + row % 16u) * 16u) = to_e4m3(a, b, byte);
   } else if (in) {
-    __builtin_nontemporal_store(to_e4m3(a, b, byte), (u32x4*)(q + row * K + k));
+    *(u32x4*)(q + row * K + k) = to_e4m3(a, b, byte);
   }
   if (here && (slot & 7u) == 0u) s[row * stride + slot / 8u] = (uint8_t)byte;
 }
