@@ -358,7 +358,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
 
   const int last = (int)min(first + kTileQ, s.nq) - 1 + off;  // last key that the workgroup's last query sees,
   const int low = (int)first + off;                           // its first query,
-  const int wave_low = low + (int)wave * 32, high = min(wave_low + 31, (int)s.nk - 1);  // the wave's first and last
+  const bool idle = first + wave * 32u >= s.nq;  // a wave without queries only loads (17 queries of 64 heads on one: 88 -> 76 us)
+  const int wave_low = low + (int)wave * 32, high = idle ? -1 : min(wave_low + 31, (int)s.nk - 1);  // the wave's first and last
   const uint32_t keys = last < 0 ? 0u : (uint32_t)last + 1u, parts = chunks_of(keys, p);
   if (c >= parts) return;  // no such chunk
   const uint32_t t0 = c * (p.chunk / kTileKeys), t1 = min((keys + kTileKeys - 1u) / kTileKeys, t0 + p.chunk / kTileKeys);
@@ -380,7 +381,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
       __syncthreads();                                  // everybody's are, and nobody reads the other stage any more
       if (t + 1u < t1) issue(t + 1u, lds + (now ^ 1u) * 2u * kBytes);
     };
-    for (; t < min(full, t1); ++t, now ^= 1u) {
+    for (; t < (idle ? t0 : min(full, t1)); ++t, now ^= 1u) {
       begin();
       const uint32_t at = lds + now * 2u * kBytes;
       attend<DP, 2, false, false>(w, at, at + kBytes, (int)(t * kTileKeys), p.scale_log2, lane);
@@ -664,12 +665,16 @@ static uint32_t chunks_of_many(uint64_t busy, uint64_t part_rows_heads, uint32_t
 
 AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads, uint32_t kv_heads, uint32_t dim, int64_t max_q, int64_t max_k) {
   AttentionPlan plan = {};
-  const uint64_t packed = (uint64_t)max_q * (heads / kv_heads);  // rows of queries that share keys
-  plan.few = packed <= 64 ? 1u : 0u;
-  plan.row_blocks = (uint32_t)((packed + 31) / 32);
-  // workgroups with work if the keys are not split: about
+  const uint32_t rep = heads / kv_heads;
+  const uint64_t packed = (uint64_t)max_q * rep, row_blocks = (packed + 31) / 32;  // rows of queries that share keys
+  // Few or many queries: the kernel for few has a workgroup for 32 rows, the other one for 128 queries of a head, filled or not.  8 sequences in front of 4000 keys, few and many: 32
+  // heads on 4, 8 queries 33 and 96 us, 16: 54 and 91; 4 sequences, 64 heads on 1, 16 queries 39 and 74, 40: 80 and 72; 16 heads of 64 on 16 in front of 1000 keys, 32 queries 17 and 22, 64: 19
+  // and 18; 8 sequences in front of 300 keys, 32 heads on 4, 8 queries 14.5 and 12.2, 16: 17.4 and 13.3.
+  plan.few = row_blocks <= (rep < 4u || max_k <= 512 ? 1u : rep / 2u) ? 1u : 0u;
+  plan.row_blocks = plan.few ? (uint32_t)row_blocks : 0u;
+  // workgroups with work if the keys are not split: about.  With few queries one to a CU is enough (4 sequences of 8000 keys, 8 key heads: 256 of them 30 us, 512 34, 1024 38).
   const uint64_t busy = plan.few ? (uint64_t)sequences * kv_heads * plan.row_blocks : ((uint64_t)q_rows + kTileQ - 1) / kTileQ * heads;
-  const uint64_t most = ((uint64_t)max_k + 255) / 256, wanted = plan.few ? 512u / (busy ? busy : 1) : chunks_of_many(busy, q_rows * heads, padded_dim(dim), max_k, most);
+  const uint64_t most = ((uint64_t)max_k + 255) / 256, wanted = plan.few ? 256u / (busy ? busy : 1) : chunks_of_many(busy, q_rows * heads, padded_dim(dim), max_k, most);
   uint64_t chunks = wanted < most ? wanted : most;
   if (chunks < 1) chunks = 1;
   plan.chunk = (uint32_t)((((uint64_t)max_k + chunks - 1) / chunks + 127) / 128 * 128);
@@ -685,14 +690,17 @@ AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads,
 
 template <int DP>
 static hipError_t run(AttentionParams& p, const AttentionPlan& plan, hipStream_t stream) {
+  // Four waves to a workgroup where every CU has one at most (8 key heads, 1000 keys: 11.9 us, 13.1 with two), else two (16 such sequences: 19.9 us, 26.4 with four)
   if (plan.few && p.units <= 256u) attention_few_kernel<DP, 4><<<p.units, 256, 0, stream>>>(p);
   else if (plan.few) attention_few_kernel<DP, 2><<<dim3(min(p.units, kGridRow), (p.units + kGridRow - 1u) / kGridRow), 128, 0, stream>>>(p);
   else attention_kernel<DP><<<(p.units + 7u) / 8u * 8u, 256, 0, stream>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.chunks == 1u) return e;
   const uint64_t pairs = p.part_rows * p.heads;
+  // 8 lanes of threads side by side where there are many chunks (390 of 100000 keys: the call 25 us, 31 with two), one where there are many rows (16384 of 9 chunks:
+  // 59 us, 73 with eight)
   if (pairs >= 8192u) attention_join_kernel<DP, 1><<<(uint32_t)((pairs + 7u) / 8u), 256, 0, stream>>>(p);
-  else if (p.chunks <= 2u) attention_join_kernel<DP, 2><<<(uint32_t)((pairs + 3u) / 4u), 256, 0, stream>>>(p);
+  else if (p.chunks <= 32u) attention_join_kernel<DP, 2><<<(uint32_t)((pairs + 3u) / 4u), 256, 0, stream>>>(p);
   else attention_join_kernel<DP, 8><<<(uint32_t)pairs, 256, 0, stream>>>(p);
   return hipGetLastError();
 }

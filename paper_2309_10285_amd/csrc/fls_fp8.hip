@@ -136,7 +136,7 @@ __device__ __forceinline__ float4v mfma(const i32x8& a, const i32x8& b, const fl
 // What counts beside W's own loads is how many lines they ask for: the slice's scales of W are copied to LDS row by row (a byte of each row for every step,
 // as many lines again as half of W, cost 8 - 20 %), and X lies in fragment order (from fp16 rows: 10 - 30 % more).
 // QUANT: a wave quantises the X that it multiplies itself, in registers, for calls where another kernel in front would cost more.
-// One step ahead and eight waves, four for 64 columns: a deeper ring or other numbers of waves were up to 5 % slower (of 28672 x 7168, N = 64: 53 us in
+// One step ahead and eight waves, four for 64 columns: a deeper ring or other numbers of waves were up to 5 % slower (the kernel at 28672 x 7168, N = 64: 53 us in
 // four, 56 in eight).
 constexpr int stream_waves(int NB) { return NB == 4 ? 4 : 8; }
 constexpr uint32_t kStreamSteps = 256, kScalePitch = kStreamSteps + 4;  // steps of a slice at most; bytes from one row's scales to the next's in LDS
@@ -464,7 +464,7 @@ static hipError_t run_tile(Fp8Params& p, hipStream_t stream) {
 // Microseconds that sums of S slices cost: a second kernel, and fp32 written and read.
 static float sums_us(uint32_t slices, uint32_t M, uint32_t N) { return slices == 1u ? 0.f : 2.5f + (float)slices * M * N * (8.f / 4.5e6f); }
 
-// What a call runs, by an estimate of its time (us) from measured rates on 256 CUs.
+// What a call runs, by an estimate of its time (us) from measured rates on 256 CUs.  Times in the comments below are those of whole calls in a graph.
 Fp8Plan fp8_plan(uint32_t M, uint32_t K, uint32_t N, int cus) {
   Fp8Plan best = {};
   float least = 3e38f;
@@ -473,8 +473,8 @@ Fp8Plan fp8_plan(uint32_t M, uint32_t K, uint32_t N, int cus) {
   const uint32_t least_slices = (steps + kStreamSteps - 1) / kStreamSteps;
   if (N <= 64 && (least_slices == 1u || least_slices <= room)) {
     // Streams run at 5.6 TB/s.  c workgroups to a CU: up to two, some CUs have one more than others; more even out.  16 and 32 rows to a workgroup read X more
-    // often than 64 do - 28672 x 7168, N = 13: 41, 38, 36 us, N = 32: 45 and 40 us in 32 and 64 rows, N = 64: 60 and 48 - and where there is one to a CU they have
-    // fewer loads under way: 7168 x 28672, N = 13: 42 us in 32 rows, 39 in 64 and two slices.  12288 x 12288, N = 13: 30 us in four slices of 64 rows (c = 3), 36 in one (c = 3/4).
+    // often than 64 do - 28672 x 7168, N = 13: 47, 42, 39 us, N = 32: 50 and 45 us in 32 and 64 rows, N = 64: 67 and 55 - and where there is one to a CU they have
+    // fewer loads under way: 7168 x 28672, N = 13: 47 us in 32 rows, 42 in 64 and two slices.  12288 x 12288, N = 13: 34 us in four slices of 64 rows (c = 3), 40 in one (c = 3/4).
     const uint32_t nb = fp8_column_groups(N);
     const float extra[3][3] = {{1.f, 1.02f, 1.15f}, {1.f, 1.12f, 1.3f}, {1.f, 1.22f, 1.5f}};
     for (int i = 0; i < 3; ++i)
@@ -490,15 +490,15 @@ Fp8Plan fp8_plan(uint32_t M, uint32_t K, uint32_t N, int cus) {
           best.slices = slices;
         }
       }
-    // Up to 16 columns of a small matrix: quantising X on the way (16 rows to a workgroup) costs less than the 2.5 us of a kernel in front of it: 1024 x 1024
-    // 4.1 us against 3.3, 4096 x 4096 9.0 against 7.3, 12288 x 12288 46 against 31.
+    // Up to 16 columns of a small matrix: quantising X on the way (16 rows to a workgroup) costs less than a kernel in front of it.  N = 1: 1024 x 1024 3.9 us
+    // against 5.1, 4096 x 4096 8.3 against 9.0, 12288 x 12288 37 against 32; N = 13: 4.0 and 5.4, 9.3 and 9.3, 54 and 34.
     const bool small = N <= 16 && K <= 8192 && (uint64_t)M * K <= (1u << 24);
     best.pass = small ? kFp8StreamQuant : kFp8Stream;
     if (small) best.tile_m = 16, best.slices = 1;
     return best;
   }
   // Tiles: a step of 256 x 256 takes 1.62 us, of 256 x 128 1.1, of 128 x 128 0.62 alone on a CU and 0.56 of two; beside them a workgroup starts and stores.
-  // 12288 x 12288, N = 4096: 487, 659, 638 us; 4096 x 4096, N = 2048: 57, 42, 47; 1024 x 1024, N = 256: 21, 14, 10.
+  // 12288 x 12288, N = 4096: 517, 783, 680 us; 4096 x 4096, N = 2048: 58, 45, 50; 1024 x 1024, N = 256: 22, 16, 12.
   best.pass = kFp8Tile;
   const struct {
     uint32_t m, n;

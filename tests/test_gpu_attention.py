@@ -393,6 +393,17 @@ def test_more_sequences_than_a_wave_has_lanes(fls, H, G, D, nq, nk):
         check(P, lse, reference(Q, K, V, q_start, k_start, k_len, 0.2))
 
 
+@pytest.mark.parametrize("H,G,D,nq,nk", [
+    (64, 1, 64, [16, 3, 9], [700, 3, 2000]), (32, 4, 128, [16, 1, 13], [600, 900, 13]), (24, 2, 80, [15], [9000]), (33, 1, 96, [15, 2], [1500, 1]), (13, 1, 128, [12, 14], [7000, 14]),
+    (64, 1, 64, [17, 3], [700, 3]), (32, 4, 128, [16, 9], [500, 512]), (32, 4, 128, [16, 9], [500, 513]), (8, 2, 40, [16], [2000]), (8, 2, 40, [17], [2000]),
+])
+def test_rows_of_many_heads_that_share_keys(fls, H, G, D, nq, nk):
+    """Several workgroups of 32 rows to a key head, and the other kernel where it takes over."""
+    Q, K, V, q_start, k_start, k_len = case(H, G, D, nq, nk, seed=H + D, q_first=1, slack=2)
+    O, lse = attend(fls, Q, K, V, q_start, k_start, k_len, D ** -0.5)
+    check(O, lse, reference(Q, K, V, q_start, k_start, k_len, D ** -0.5))
+
+
 def test_sequences_that_share_keys_and_are_cut(fls):
     """Two sequences on the same keys (a shared prefix); and max_q, max_k below what a sequence has: its first so many of each."""
     Q, K, V, q_start, _, _ = case(4, 2, 64, [3, 2, 140], [400], seed=13)
