@@ -61,10 +61,10 @@ __device__ __forceinline__ u32x4 to_e4m3(const u32x4& a, const u32x4& b, uint32_
 }
 
 // Rows of fp16 -> e4m3 [rows][K] and scales [rows][stride].  Bound by memory: 2 bytes in, 1 out.  A lane takes 16 values (32 B in,
-// 16 B out), the eight lanes of a block agree on its largest.  Blocks from K on, up to the stride, have a scale of one.  Loads that the caches need not keep and
-// ordinary stores: 28672 x 7168 96 us, 6.4 TB/s; both ordinary 106, neither kept 102.
+// 16 B out), the eight lanes of a block agree on its largest.  Blocks from K on, up to the stride, have a scale of one.  The caches need not keep what
+// is read; what is written they keep where a product follows (KEEP: 12288 x 12288, N = 4096 1 % less), not where a matrix is quantised once (28672 x 7168 102 us, 6.1 TB/s; kept 106).
 // FRAGMENTS: the values as the stream kernel reads them, [step][16 rows][half][lane][16] with `columns` groups of 16 rows, whole steps.
-template <bool FRAGMENTS>
+template <bool FRAGMENTS, bool KEEP>
 __global__ __launch_bounds__(256) void quantize_kernel(const _Float16* W, uint8_t* q, uint8_t* s, uint32_t K, uint32_t stride, Divisor by_slots, uint64_t rows, uint32_t columns) {
   // blocks of a grid row cover kQuantizeRows rows, so that the division is one of small numbers
   const uint64_t row0 = (uint64_t)blockIdx.y * kQuantizeRows;
@@ -93,7 +93,9 @@ __global__ __launch_bounds__(256) void quantize_kernel(const _Float16* W, uint8_
     if (here && step * kBlock < K)
       *(u32x4*)(q + (((uint64_t)step * columns + row / 16u) * 2u + piece % 2u) * 1024u + (piece / 2u * 16u + row % 16u) * 16u) = to_e4m3(a, b, byte);
   } else if (in) {
-    *(u32x4*)(q + row * K + k) = to_e4m3(a, b, byte);
+    const u32x4 v = to_e4m3(a, b, byte);
+    if (KEEP) *(u32x4*)(q + row * K + k) = v;
+    else __builtin_nontemporal_store(v, (u32x4*)(q + row * K + k));
   }
   if (here && (slot & 7u) == 0u) s[row * stride + slot / 8u] = (uint8_t)byte;
 }
@@ -431,17 +433,17 @@ __global__ __launch_bounds__(256) void fp8_sum_kernel(const float* parts, _Float
 
 // --- host ---------------------------------------------------------------------------------------------------------------------
 
-template <bool FRAGMENTS>
+template <bool FRAGMENTS, bool KEEP>
 static hipError_t run_quantize(const _Float16* W, uint8_t* q, uint8_t* s, uint64_t rows, uint32_t K, uint32_t columns, hipStream_t stream) {
   const uint32_t stride = scale_stride(K), slots = stride * 8u;
   const uint64_t a_row = rows < kQuantizeRows ? rows : kQuantizeRows;
   const dim3 grid((uint32_t)((a_row * slots + 255u) / 256u), (uint32_t)((rows + kQuantizeRows - 1) / kQuantizeRows));
-  quantize_kernel<FRAGMENTS><<<grid, 256, 0, stream>>>(W, q, s, K, stride, divisor(slots), rows, columns);
+  quantize_kernel<FRAGMENTS, KEEP><<<grid, 256, 0, stream>>>(W, q, s, K, stride, divisor(slots), rows, columns);
   return hipGetLastError();
 }
 
 hipError_t launch_quantize(const _Float16* W, uint8_t* q, uint8_t* s, uint64_t rows, uint32_t K, hipStream_t stream) {
-  return run_quantize<false>(W, q, s, rows, K, 0, stream);
+  return run_quantize<false, false>(W, q, s, rows, K, 0, stream);
 }
 
 template <int RB, int NB, bool QUANT>
@@ -535,8 +537,8 @@ hipError_t launch_fp8(const Fp8Launch& a, hipStream_t stream) {
   p.slices = plan.slices;
   p.by_slices = divisor(plan.slices);
   hipError_t e = hipSuccess;
-  if (plan.pass == kFp8Stream) e = run_quantize<true>(a.X, a.Xq, a.Xs, a.N, a.K, fp8_column_groups(a.N), stream);
-  else if (plan.pass == kFp8Tile) e = run_quantize<false>(a.X, a.Xq, a.Xs, a.N, a.K, 0, stream);
+  if (plan.pass == kFp8Stream) e = run_quantize<true, true>(a.X, a.Xq, a.Xs, a.N, a.K, fp8_column_groups(a.N), stream);
+  else if (plan.pass == kFp8Tile) e = run_quantize<false, true>(a.X, a.Xq, a.Xs, a.N, a.K, 0, stream);
   if (e != hipSuccess) return e;
   if (plan.pass == kFp8StreamQuant) e = run_stream<1, 1, true>(p, stream);
   else if (plan.pass == kFp8Stream)
