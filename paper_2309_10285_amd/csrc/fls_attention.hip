@@ -295,7 +295,9 @@ __device__ __forceinline__ float log_sum(float m, float l) { return l > 0.f ? (m
 
 // --- many queries to a sequence ------------------------------------------------------------------------------------------------
 // A workgroup has 128 queries of a head, 32 to a wave; tiles of 64 keys go through LDS in two stages.  Tiles that every query sees
-// come first, in a loop without a mask.
+// come first, in a loop without a mask.  A prompt of 8192, 64 heads of 128 on 8: 1127 us, 0.98 PFLOP/s, bound by power (1.8 GHz; 864 us with all inputs zero).  Eight prompts of
+// 17 - 1500, 56 heads of 128: 209 us, of which queries and results 35: a workgroup's start and end find only one other on its CU to hide behind (64 KB of LDS and 256
+// registers allow two).
 
 constexpr uint32_t kTileQ = 128, kTileKeys = 64;
 
@@ -451,7 +453,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
 }
 
 // --- few queries to a sequence -------------------------------------------------------------------------------------------------
-// Bound by the stream of keys and values (loads that the caches do not keep: 64 tokens, 56 heads, 345 -> 313 us).  The queries of all heads that share a key head are the 32 columns of a wave; a workgroup has
+// Bound by the stream of keys and values (loads that the caches do not keep: 64 tokens behind 300 - 2047 keys, 56 heads of 128, 345 -> 313 us, 6.1 TB/s).  The queries of all heads that share a key head are the 32 columns of a wave; a workgroup has
 // a chunk of a sequence's keys, its waves take tiles of 32 in turn, each with two stages of its own in LDS and no barrier, and add
 // up what they have at the end.
 
