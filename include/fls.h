@@ -178,7 +178,7 @@ int fls_check_workspace(fls_stream_t stream);
  * validate it and to pick the kernel variant; later calls on that address do not.  Call
  * fls_forget when the memory at that address comes to hold a different blob by other means than
  * fls_compress (a copy, a freed buffer handed out again).  A remembered header that is out of date
- * but of the same M, K costs speed only (a variant sized for other tile lengths, down to a plain
+ * but of the same M, K and format version costs speed only (a variant sized for other tile lengths, down to a plain
  * slow path); the kernels take every tile's length from the blob itself.
  * Stream capture: a call on a blob address the library already knows enqueues kernels only (no
  * copies, no memsets, no host-side per-launch state in their arguments), so it may be recorded

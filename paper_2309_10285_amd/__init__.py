@@ -13,6 +13,7 @@ import ctypes
 import operator
 import os
 import struct
+import weakref
 
 TILE_M = 128
 TILE_K = 32
@@ -151,6 +152,16 @@ def _check(rc, where):
         raise FlsError(rc, where)
 
 
+def _new_blob(W, bound):
+    """Memory for a compressed W.  The library remembers the address until the memory goes back to torch's allocator, which hands it out again for something else:
+    an entry of the other format version would be read wrongly."""
+    import torch
+
+    out = torch.empty(bound, dtype=torch.uint8, device=W.device)
+    weakref.finalize(out.untyped_storage(), lib().fls_forget, out.data_ptr()).atexit = False
+    return out
+
+
 def fls_compress_bound(M, K):
     out = ctypes.c_size_t(0)
     _check(lib().fls_compress_bound(M, K, ctypes.byref(out)), "fls_compress_bound")
@@ -200,7 +211,7 @@ def fls_compress(W, out=None, order_policy=ORDER_LOCATION):
     assert W.is_cuda and W.dtype == torch.float16 and W.is_contiguous() and W.dim() == 2
     M, K = W.shape
     if out is None:
-        out = torch.empty(fls_compress_bound(M, K), dtype=torch.uint8, device=W.device)
+        out = _new_blob(W, fls_compress_bound(M, K))
     st = FlsStats()
     rc = lib().fls_compress(W.data_ptr(), M, K, out.data_ptr(), out.numel(),
                             order_policy, ctypes.byref(st), _stream())
@@ -221,7 +232,7 @@ def fls_compress_v2(W, out=None):
     assert W.is_cuda and W.dtype == torch.float16 and W.is_contiguous() and W.dim() == 2
     M, K = W.shape
     if out is None:
-        out = torch.empty(fls_compress_bound_v2(M, K), dtype=torch.uint8, device=W.device)
+        out = _new_blob(W, fls_compress_bound_v2(M, K))
     st = FlsStats()
     rc = lib().fls_compress_v2(W.data_ptr(), M, K, out.data_ptr(), out.numel(),
                                ctypes.byref(st), _stream())
