@@ -297,7 +297,8 @@ __device__ __forceinline__ float log_sum(float m, float l) { return l > 0.f ? (m
 // A workgroup has 128 queries of a head, 32 to a wave; tiles of 64 keys go through LDS in two stages.  Tiles that every query sees
 // come first, in a loop without a mask.  A prompt of 8192, 64 heads of 128 on 8: 1127 us, 0.98 PFLOP/s, bound by power (1.8 GHz; 864 us with all inputs zero).  Eight prompts of
 // 17 - 1500, 56 heads of 128: 209 us, of which queries and results 35: a workgroup's start and end find only one other on its CU to hide behind (64 KB of LDS and 256
-// registers allow two).
+// registers allow two).  With rows of 64 values three fit, in 32 KB and 168 registers: 8 prompts of 1024, 56 heads of 64, 119 -> 112 us, 64 of 128 63 -> 55, one of 8192 617 -> 589.  (Tiles of
+// 32 keys would let three of 128 values fit but for registers: 135 spilled, 193 -> 315 us; two of them 193 -> 206.)
 
 constexpr uint32_t kTileQ = 128, kTileKeys = 64;
 
@@ -313,7 +314,7 @@ __device__ __forceinline__ uint32_t sum_up_to_lane(uint32_t x) {
 }
 
 template <int DP>
-__global__ __launch_bounds__(256, 2) void attention_kernel(AttentionParams p) {
+__global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attention_kernel(AttentionParams p) {
   constexpr int kBytes = kTileKeys * kPitch<DP> * 2;
   __shared__ __align__(16) uint8_t stages[2][2 * kBytes];  // a tile of K, one of V
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
