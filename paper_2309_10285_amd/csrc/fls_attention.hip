@@ -294,13 +294,12 @@ __device__ __forceinline__ void store_rows(const Wave<DP>& w, _Float16* row, flo
 __device__ __forceinline__ float log_sum(float m, float l) { return l > 0.f ? (m - kLift + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : l == 0.f ? -kInf : l; }
 
 // --- many queries to a sequence ------------------------------------------------------------------------------------------------
-// A workgroup has 128 queries of a head, 32 to a wave; tiles of 64 keys go through LDS in two stages.  Tiles that every query sees
+// A workgroup has 128 queries of a head, 32 to a wave; tiles of 32 or 64 keys go through LDS in two stages.  Tiles that every query sees
 // come first, in a loop without a mask.  A prompt of 8192, 64 heads of 128 on 8: 1127 us, 0.98 PFLOP/s, bound by power (1.8 GHz; 864 us with all inputs zero).  Eight prompts of
-// 17 - 1500, 56 heads of 128: 209 us, of which queries and results 35: a workgroup's start and end find only one other on its CU to hide behind (64 KB of LDS and 256
-// registers allow two).  With rows of 64 values three fit, in 32 KB and 168 registers: 8 prompts of 1024, 56 heads of 64, 119 -> 112 us, 64 of 128 63 -> 55, one of 8192 617 -> 589.  (Tiles of
-// 32 keys would let three of 128 values fit but for registers: 135 spilled, 193 -> 315 us; two of them 193 -> 206.)
+// 17 - 1500, 56 heads of 128: 194 us, of which queries and results some 30: a workgroup's start and end have only the others on its CU to hide behind.  Two fit in 64 KB of LDS each and 256
+// registers; three in 32 KB and 168 registers, with rows of 64 values (8 prompts of 1024, 56 heads of 64, 119 -> 112 us, 64 of 128 63 -> 55) or tiles of 32 keys.
 
-constexpr uint32_t kTileQ = 128, kTileKeys = 64;
+constexpr uint32_t kTileQ = 128;
 
 // x of all lanes up to this one.
 __device__ __forceinline__ uint32_t sum_up_to_lane(uint32_t x) {
@@ -313,9 +312,9 @@ __device__ __forceinline__ uint32_t sum_up_to_lane(uint32_t x) {
   return x;
 }
 
-template <int DP>
-__global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attention_kernel(AttentionParams p) {
-  constexpr int kBytes = kTileKeys * kPitch<DP> * 2;
+template <int DP, int KEYS>
+__global__ __launch_bounds__(256, KEYS * kPitch<DP> <= 4096 ? 3 : 2) void attention_kernel(AttentionParams p) {
+  constexpr int B = KEYS / 32, kBytes = KEYS * kPitch<DP> * 2;
   __shared__ __align__(16) uint8_t stages[2][2 * kBytes];  // a tile of K, one of V
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t unit;
@@ -365,62 +364,67 @@ __global__ __launch_bounds__(256, DP == 64 ? 3 : 2) void attention_kernel(Attent
   const int wave_low = low + (int)wave * 32, high = idle ? -1 : min(wave_low + 31, (int)s.nk - 1);  // the wave's first and last
   const uint32_t keys = last < 0 ? 0u : (uint32_t)last + 1u, parts = chunks_of(keys, p);
   if (c >= parts) return;  // no such chunk
-  const uint32_t t0 = c * (p.chunk / kTileKeys), t1 = min((keys + kTileKeys - 1u) / kTileKeys, t0 + p.chunk / kTileKeys);
-  const uint32_t full = low < 0 ? 0u : ((uint32_t)low + 1u) / kTileKeys;  // tiles that all see (the same for all waves)
+  const uint32_t t0 = c * (p.chunk / KEYS), t1 = min((keys + KEYS - 1u) / KEYS, t0 + p.chunk / KEYS);
+  const uint32_t full = low < 0 ? 0u : ((uint32_t)low + 1u) / KEYS;  // tiles that all see (the same for all waves)
   auto issue = [&](uint32_t t, uint32_t to) {
-    const int64_t row = s.k0 + (int64_t)t * kTileKeys;
-    const uint32_t left = s.nk - t * kTileKeys;
-    stage<DP, kTileKeys, 256>(p.K + row * p.k_row + (int64_t)g * p.k_head, p.k_row, left, p.dim, to, threadIdx.x);
-    stage<DP, kTileKeys, 256>(p.V + row * p.v_row + (int64_t)g * p.v_head, p.v_row, left, p.dim, to + kBytes, threadIdx.x);
+    const int64_t row = s.k0 + (int64_t)t * KEYS;
+    const uint32_t left = s.nk - t * KEYS;
+    stage<DP, KEYS, 256>(p.K + row * p.k_row + (int64_t)g * p.k_head, p.k_row, left, p.dim, to, threadIdx.x);
+    stage<DP, KEYS, 256>(p.V + row * p.v_row + (int64_t)g * p.v_head, p.v_row, left, p.dim, to + kBytes, threadIdx.x);
   };
   const uint32_t lds = lds_at(stages);
   if (t0 < t1) issue(t0, lds);
-  w.load(p.Q + (s.q0 + mine) * p.q_row + (int64_t)head * p.q_head, here, p.dim, lane);
+  const _Float16* q_row = p.Q + (s.q0 + mine) * p.q_row + (int64_t)head * p.q_head;
+  w.load(q_row, here, p.dim, lane);
   __builtin_amdgcn_s_waitcnt(0);  // the compiler's loads have come: it has nothing to wait for among the loop's
-  for (bool careful = false;; careful = true) {
-    uint32_t t = t0, now = 0;
-    auto begin = [&]() {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's pieces of the tile are in LDS
-      __syncthreads();                                  // everybody's are, and nobody reads the other stage any more
-      if (t + 1u < t1) issue(t + 1u, lds + (now ^ 1u) * 2u * kBytes);
-    };
-    for (; t < (idle ? t0 : min(full, t1)); ++t, now ^= 1u) {
-      begin();
-      const uint32_t at = lds + now * 2u * kBytes;
-      attend<DP, 2, false, false>(w, at, at + kBytes, (int)(t * kTileKeys), p.scale_log2, lane);
-    }
-    for (; t < t1; ++t, now ^= 1u) {
-      begin();
-      const uint32_t at = lds + now * 2u * kBytes;
-      const int key0 = (int)(t * kTileKeys);
-      if (key0 > high) continue;
-      if (key0 + (int)kTileKeys - 1 <= wave_low) {
-        attend<DP, 2, false, false>(w, at, at + kBytes, key0, p.scale_log2, lane);
-      } else if (!careful) {
-        attend<DP, 2, true, false>(w, at, at + kBytes, key0, p.scale_log2, lane);
-      } else {
+  uint32_t t = t0, now = 0;
+  auto begin = [&]() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's pieces of the tile are in LDS
+    __syncthreads();                                  // everybody's are, and nobody reads the other stage any more
+    if (t + 1u < t1) issue(t + 1u, lds + (now ^ 1u) * 2u * kBytes);
+  };
+  for (; t < (idle ? t0 : min(full, t1)); ++t, now ^= 1u) {
+    begin();
+    const uint32_t at = lds + now * 2u * kBytes;
+    attend<DP, B, false, false>(w, at, at + kBytes, (int)(t * KEYS), p.scale_log2, lane);
+  }
+  for (; t < t1; ++t, now ^= 1u) {
+    begin();
+    const uint32_t at = lds + now * 2u * kBytes;
+    const int key0 = (int)(t * KEYS);
+    if (key0 <= high) attend<DP, B, true, false>(w, at, at + kBytes, key0, p.scale_log2, lane);
+  }
+  // Sums that are not finite may come from values that a query does not see, times a weight of 0.  That is found here, once, and then all is done again with
+  // an eye on them: to look at every tile's values cost a tenth of short prompts.  A loop of its own, queries read again: what it needs in registers (and spills), the loops above need not
+  // have (as one loop that runs twice: 8 prompts of 1024 200 us instead of 196).
+  float odd = 0.f;  // NaN, if one is not finite
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) odd = __builtin_fmaf(w.o[d][i], 0.f, odd);
+  if (__syncthreads_or(odd != 0.f && full < t1)) {
+    w.clear();
+    w.load(q_row, here, p.dim, lane);
+    __builtin_amdgcn_s_waitcnt(0);
+    issue(t0, lds);
+    now = 0;
 #pragma unroll 1
-        for (uint32_t half = 0; half < 2u; ++half)
-          attend<DP, 1, true, true>(w, at + half * (kBytes / 2), at + kBytes + half * (kBytes / 2), key0 + (int)half * 32, p.scale_log2, lane);
+    for (t = t0; t < t1; ++t, now ^= 1u) {
+      begin();
+#pragma unroll 1
+      for (uint32_t b = 0; b < (uint32_t)B; ++b) {
+        const uint32_t at = lds + now * 2u * kBytes + b * (kBytes / B);
+        const int key0 = (int)(t * KEYS + b * 32u);
+        if (key0 <= high) attend<DP, 1, true, true>(w, at, at + kBytes, key0, p.scale_log2, lane);
       }
     }
-    // Sums that are not finite may come from values that a query does not see, times a weight of 0.  That is found here, once, and then all is done again with
-    // an eye on them: to look at every tile's values cost a tenth of short prompts.
-    float most = 0.f;
-#pragma unroll
-    for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) most = fmaxf(most, w.o[d][i] - w.o[d][i] == 0.f ? 0.f : 1.f);
-    if (careful || full >= t1 || !__syncthreads_or(most != 0.f)) break;
-    w.clear();
-    issue(t0, lds);
+    __syncthreads();
   }
   w.l = across(w.l, true);
   const int64_t row = s.q0 + mine;
   if (parts == 1u) {
     // Through LDS, so that 16 (8) lanes write a row: stores of the 8 bytes that a lane has of its query took a seventh of short prompts' time.  The caches
     // need not keep it (64 prompts of 128, 56 heads: 110.8 -> 107.7 us).  Queries gain nothing from coming in whole rows through LDS (124).
-    __syncthreads();  // nobody reads a tile any more
     constexpr uint32_t kRow = kPitch<DP> * 2, kPieces = kPitch<DP> / 8;
     const uint32_t mine_at = lds + wave * 32u * kRow;
     const float factor = w.l > 0.f ? 1.f / w.l : w.l;
@@ -697,7 +701,10 @@ static hipError_t run(AttentionParams& p, const AttentionPlan& plan, hipStream_t
   // Four waves to a workgroup where every CU has one at most (8 key heads, 1000 keys: 11.9 us, 13.1 with two), else two (16 such sequences: 19.9 us, 26.4 with four)
   if (plan.few && p.units <= 256u) attention_few_kernel<DP, 4><<<p.units, 256, 0, stream>>>(p);
   else if (plan.few) attention_few_kernel<DP, 2><<<dim3(min(p.units, kGridRow), (p.units + kGridRow - 1u) / kGridRow), 128, 0, stream>>>(p);
-  else attention_kernel<DP><<<(p.units + 7u) / 8u * 8u, 256, 0, stream>>>(p);
+  // Tiles of 32 keys where heads have 128 values and there are more than four workgroups to a CU, none of them long: 8 prompts of 1024, 56 heads, 181 us, 196 with 64; 16 of 512 123 and 129; 4 of
+  // 2048 303 and 308; 2 of 4096 553 and 549; one of 8192 1050 and 1035; 512 queries behind 2000 keys, 64 heads (512 workgroups) 77 and 63.
+  else if (DP == 128 && p.units > 1024u && p.max_k <= 2048u) attention_kernel<DP, DP == 128 ? 32 : 64><<<(p.units + 7u) / 8u * 8u, 256, 0, stream>>>(p);
+  else attention_kernel<DP, 64><<<(p.units + 7u) / 8u * 8u, 256, 0, stream>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.chunks == 1u) return e;
   const uint64_t pairs = p.part_rows * p.heads;

@@ -404,6 +404,31 @@ def test_rows_of_many_heads_that_share_keys(fls, H, G, D, nq, nk):
     check(O, lse, reference(Q, K, V, q_start, k_start, k_len, D ** -0.5))
 
 
+@pytest.mark.parametrize("D", [128, 104])
+@pytest.mark.parametrize("G", [64, 16])
+def test_many_workgroups(fls, D, G):
+    """More than four workgroups to a CU, with tiles of their own: ragged lengths, fewer keys than queries, none, and values that are not finite in keys that are not seen or seen by some."""
+    import random
+
+    import torch
+
+    r = random.Random(D + G)
+    nq = [r.choice((0, 1, 33, 128, 129, 200, r.randint(2, 260))) for _ in range(22)] + [100, 150]
+    nk = [max(0, n + r.choice((0, 0, 1, 31, 64, 700, -n // 2, -n))) for n in nq[:-2]] + [100, 2048]
+    Q, K, V, q_start, k_start, k_len = case(64, G, D, nq, nk, seed=D, q_first=1, slack=3)
+    O, lse = attend(fls, Q, K, V, q_start, k_start, k_len, 0.1)
+    check(O, lse, reference(Q, K, V, q_start, k_start, k_len, 0.1))
+    outside = torch.ones(K.shape[0], dtype=torch.bool, device="cuda")
+    for at, n in zip(k_start, k_len):
+        outside[at:at + n] = False
+    K[outside], V[outside] = math.nan, math.inf
+    for b in (22, 23):  # keys that the last few queries see
+        last = k_start[b] + k_len[b] - 1
+        V[last, 3, 7], V[last - 1, 5, 8], V[last - 40, 7, 9], K[last - 2, 0] = math.inf, math.nan, -math.inf, -1000.0
+    O, lse = attend(fls, Q, K, V, q_start, k_start, k_len, 0.1)
+    check(O, lse, reference(Q, K, V, q_start, k_start, k_len, 0.1))
+
+
 def test_sequences_that_share_keys_and_are_cut(fls):
     """Two sequences on the same keys (a shared prefix); and max_q, max_k below what a sequence has: its first so many of each."""
     Q, K, V, q_start, _, _ = case(4, 2, 64, [3, 2, 140], [400], seed=13)
