@@ -189,19 +189,28 @@ def fls_set_workspace(ws):
 
 
 def ensure_workspace(M, K, N):
-    """Registers a (torch-allocated) workspace large enough for this shape if the current one is not."""
+    """Registers a (torch-allocated) workspace large enough for this shape if the current one is not; not while a graph is recorded, unless it is large enough already."""
+    need = lib().fls_workspace_bytes(M, K, N)
+    if need == 0 or _ws_tensor is None or _ws_tensor.numel() < need:
+        _ensure(need, "fls_workspace_bytes")
+
+
+def _ensure(need, where):
     import torch
 
-    need = fls_workspace_bytes(M, K, N)
     if need == 0:
-        raise FlsError(EINVAL, "fls_workspace_bytes")
-    if _ws_tensor is None or _ws_tensor.numel() < need:
-        _make_workspace(torch.empty(need, dtype=torch.uint8, device="cuda"))
-
-
-def _make_workspace(ws):
+        raise FlsError(EINVAL, where)
+    if torch.cuda.is_current_stream_capturing():  # memory of the graph's own, cleared in each replay
+        raise FlsError(EWORKSPACE, where)
+    # a power of two, and one of each: all that were ever made are together less than twice the largest, four times what was needed at most
+    size = 1 << (need - 1).bit_length()
+    for ws in _ws_made:  # a caller's own was registered since
+        if ws.numel() == size and (not _several_devices or _on_this_device(ws)):
+            break
+    else:
+        ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+        _ws_made.append(ws)
     fls_set_workspace(ws)
-    _ws_made.append(ws)
 
 
 def fls_compress(W, out=None, order_policy=ORDER_LOCATION):
@@ -399,18 +408,6 @@ def fls_quantize(W, out=None):
 
 def fls_fp8_workspace_bytes(M, K, N):
     return int(lib().fls_fp8_workspace_bytes(M, K, N))
-
-
-def _ensure(need, where):
-    import torch
-
-    if need == 0:
-        raise FlsError(EINVAL, where)
-    if _ws_tensor is None or _ws_tensor.numel() < need:
-        if torch.cuda.is_current_stream_capturing():  # memory of the graph's own, cleared in each replay
-            raise FlsError(EWORKSPACE, where)
-        # a power of two: all that were ever made are no more than twice the largest
-        _make_workspace(torch.empty(1 << (need - 1).bit_length(), dtype=torch.uint8, device="cuda"))
 
 
 def _on_this_device(*tensors):
