@@ -152,14 +152,23 @@ def _check(rc, where):
         raise FlsError(rc, where)
 
 
-def _new_blob(W, bound):
-    """Memory for a compressed W.  The library remembers the address until the memory goes back to torch's allocator, which hands it out again for something else:
-    an entry of the other format version would be read wrongly."""
-    import torch
+_forgets = {}  # address of a blob -> the finalizer of its memory
 
-    out = torch.empty(bound, dtype=torch.uint8, device=W.device)
-    weakref.finalize(out.untyped_storage(), lib().fls_forget, out.data_ptr()).atexit = False
-    return out
+
+def _forget_when_freed(blob):
+    """The library remembers a blob's address until the memory goes back to torch's allocator, which hands it out again for something else: an entry of the
+    other format version would be read wrongly.  What is copied over a blob in memory that stays is for fls_forget."""
+    storage, at = blob.untyped_storage(), blob.data_ptr()
+    known = _forgets.get(at)
+    alive = known.peek() if known is not None else None
+    if alive is None or alive[0] is not storage:
+        _forgets[at] = end = weakref.finalize(storage, _freed, at)
+        end.atexit = False
+
+
+def _freed(at):
+    _forgets.pop(at, None)
+    lib().fls_forget(at)
 
 
 def fls_compress_bound(M, K):
@@ -220,7 +229,8 @@ def fls_compress(W, out=None, order_policy=ORDER_LOCATION):
     assert W.is_cuda and W.dtype == torch.float16 and W.is_contiguous() and W.dim() == 2
     M, K = W.shape
     if out is None:
-        out = _new_blob(W, fls_compress_bound(M, K))
+        out = torch.empty(fls_compress_bound(M, K), dtype=torch.uint8, device=W.device)
+    _forget_when_freed(out)
     st = FlsStats()
     rc = lib().fls_compress(W.data_ptr(), M, K, out.data_ptr(), out.numel(),
                             order_policy, ctypes.byref(st), _stream())
@@ -241,7 +251,8 @@ def fls_compress_v2(W, out=None):
     assert W.is_cuda and W.dtype == torch.float16 and W.is_contiguous() and W.dim() == 2
     M, K = W.shape
     if out is None:
-        out = _new_blob(W, fls_compress_bound_v2(M, K))
+        out = torch.empty(fls_compress_bound_v2(M, K), dtype=torch.uint8, device=W.device)
+    _forget_when_freed(out)
     st = FlsStats()
     rc = lib().fls_compress_v2(W.data_ptr(), M, K, out.data_ptr(), out.numel(),
                                ctypes.byref(st), _stream())
@@ -255,7 +266,10 @@ def fls_spmm(blob, X, C, M, K, N):
     assert blob.is_cuda and blob.dtype == torch.uint8 and blob.is_contiguous()
     assert X.is_cuda and X.dtype == torch.float16 and X.is_contiguous() and X.shape == (N, K)
     assert C.is_cuda and C.dtype == torch.float16 and C.is_contiguous() and C.shape == (N, M)
-    _check(lib().fls_spmm(blob.data_ptr(), X.data_ptr(),
+    at = blob.data_ptr()
+    if at not in _forgets:
+        _forget_when_freed(blob)
+    _check(lib().fls_spmm(at, X.data_ptr(),
                           C.data_ptr(), M, K, N, _stream()), "fls_spmm")
     return C
 
@@ -298,6 +312,7 @@ def prepare_spmm(blob, X, C, M, K, N):
     assert X.is_cuda and X.dtype == torch.float16 and X.is_contiguous() and X.shape == (N, K)
     assert C.is_cuda and C.dtype == torch.float16 and C.is_contiguous() and C.shape == (N, M)
     f = lib().fls_spmm
+    _forget_when_freed(blob)
     args = (blob.data_ptr(), X.data_ptr(), C.data_ptr(),
             M, K, N, _stream())
     keep = (blob, X, C)  # the tensors stay alive as long as the callable does

@@ -48,3 +48,43 @@ def test_a_blob_of_the_other_version_in_memory_that_was_freed(fls, N):
     fls.fls_spmm(place, X, C, M, K, N)
     assert close()
     fls.fls_forget(place)
+
+
+@pytest.mark.parametrize("N", [8, 48, 200])
+@pytest.mark.parametrize("how", ["out", "copy", "prepared"])
+def test_a_blob_that_the_caller_placed(fls, how, N):
+    """The same for memory that the caller gave fls_compress, and for a copy of a blob that the library saw in a product first."""
+    import torch
+
+    M, K = 640, 3040
+    gen = torch.Generator(device="cuda").manual_seed(N + len(how))
+    W = torch.randn(M, K, generator=gen, device="cuda").half()
+    W[torch.rand(M, K, generator=gen, device="cuda") < 0.7] = 0
+    X, C = torch.randn(N, K, generator=gen, device="cuda").half(), torch.empty(N, M, dtype=torch.float16, device="cuda")
+    ref = X.double() @ W.double().T
+    close = lambda: ((C.double() - ref).abs().max() <= 2e-3 * ref.abs().max()).item()  # noqa: E731
+    fls.ensure_workspace(M, K, N)
+    blobs = [fls.fls_compress(W)[0], fls.fls_compress_v2(W)[0]]
+    size, address, held = fls.fls_compress_bound(M, K), None, []
+    for version in (0, 1, 0, 1):
+        for _ in range(50):
+            place = torch.empty(size, dtype=torch.uint8, device="cuda")
+            if address in (None, place.data_ptr()):
+                break
+            held.append(place)
+        else:
+            pytest.skip("the allocator did not hand the memory out again")
+        address = place.data_ptr()
+        if how == "out" and version == 0:
+            fls.fls_compress(W, out=place)
+        else:
+            place[:blobs[version].numel()].copy_(blobs[version])
+        C.zero_()
+        if how == "prepared":
+            call = fls.prepare_spmm(place, X, C, M, K, N)
+            call()
+            del call
+        else:
+            fls.fls_spmm(place, X, C, M, K, N)
+        assert close()
+        del place
