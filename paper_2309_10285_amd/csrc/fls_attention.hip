@@ -124,7 +124,9 @@ __device__ __forceinline__ float across(float x, bool add) {  // with the lane 3
 }
 
 // Where a lane begins to read in a tile of K or V, from its start on.  All its other places differ from that in bits that pieces lie in (and in whole rows), so
-// they are one exclusive or away: kept in registers, they would be more than there are.
+// they are one exclusive or away: kept in registers, they would be more than there are.  That is right for the address in LDS as well if no bit of the tile's
+// start is among them: tiles begin at multiples of kTileAlign.
+constexpr uint32_t kTileAlign = 256;  // a row of 128 values
 template <int DP>
 __device__ __forceinline__ uint32_t key_place(uint32_t lane) {
   const uint32_t row = lane & 31u;
@@ -315,7 +317,8 @@ __device__ __forceinline__ uint32_t sum_up_to_lane(uint32_t x) {
 template <int DP, int KEYS>
 __global__ __launch_bounds__(256, KEYS * kPitch<DP> <= 4096 ? 3 : 2) void attention_kernel(AttentionParams p) {
   constexpr int B = KEYS / 32, kBytes = KEYS * kPitch<DP> * 2;
-  __shared__ __align__(16) uint8_t stages[2][2 * kBytes];  // a tile of K, one of V
+  __shared__ __align__(kTileAlign) uint8_t stages[2][2 * kBytes];  // a tile of K, one of V
+  static_assert(__alignof__(stages) % kTileAlign == 0 && kBytes / B % kTileAlign == 0, "tiles, and blocks of 32 keys in them");
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t unit;
   if (!xcd_unit(p.units, unit)) return;
@@ -468,7 +471,8 @@ constexpr uint32_t kGridRow = 1u << 23;  // workgroups: a grid has less than 2^3
 template <int DP, uint32_t WAVES>
 __global__ __launch_bounds__(WAVES * 64) void attention_few_kernel(AttentionParams p) {
   constexpr int kBytes = kFewKeys * kPitch<DP> * 2;
-  __shared__ __align__(16) uint8_t stage0[WAVES][2 * kBytes], stage1[WAVES][2 * kBytes];
+  __shared__ __align__(kTileAlign) uint8_t stage0[WAVES][2 * kBytes], stage1[WAVES][2 * kBytes];
+  static_assert(__alignof__(stage0) % kTileAlign == 0 && __alignof__(stage1) % kTileAlign == 0 && kBytes % kTileAlign == 0, "tiles");
   __shared__ float top[WAVES][32], sum[WAVES][32];
   const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // chunk outermost: sequences of one length run side by side
