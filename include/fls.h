@@ -306,7 +306,7 @@ typedef struct {
 #define FLS_MAX_HEAD_DIM 128
 
 /* Bytes of device workspace fls_attention needs for this shape: the control area of fls_workspace_bytes and, where a sequence's keys are
- * shared out among workgroups because there are few queries, their sums.  Returns 0 on invalid arguments. */
+ * shared out among workgroups because there are few queries, their sums (how many depends on the GPU's CUs).  Returns 0 on invalid arguments. */
 size_t fls_attention_workspace_bytes(const fls_attention_shape* shape_host);
 
 /*

@@ -113,6 +113,8 @@ def lib():
         L.fls_attention.restype = ci
         L.fls_internal_fp8_plan.argtypes = [ctypes.c_uint32] * 3 + [ci, ctypes.POINTER(ctypes.c_uint32)]
         L.fls_internal_fp8_plan.restype = None
+        L.fls_internal_attention_plan.argtypes = [i64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, i64, i64, ci, ctypes.POINTER(ctypes.c_uint32)]
+        L.fls_internal_attention_plan.restype = None
         L.fls_internal_spmm_plan.argtypes = [ctypes.c_uint32] * 5 + [ci, ci, ctypes.POINTER(ctypes.c_uint32)]
         L.fls_internal_spmm_plan.restype = None
         L.fls_strerror.argtypes = [ci]

@@ -628,7 +628,9 @@ static bool attention_shape_ok(const fls_attention_shape* s, fls::AttentionPlan*
   const bool head_of_rows = (s->q_rows <= 1 || s->o_row >= s->head_dim) && (s->heads == 1 || s->o_head >= (s->q_rows - 1) * s->o_row + s->head_dim);
   if (!row_of_heads && !head_of_rows) return false;
   const int64_t max_q = s->max_q < s->q_rows ? s->max_q : s->q_rows, max_k = s->max_k < s->k_rows ? s->max_k : s->k_rows;
-  *plan = fls::attention_plan(s->q_rows, (uint32_t)s->sequences, (uint32_t)s->heads, (uint32_t)s->kv_heads, (uint32_t)s->head_dim, max_q, max_k);
+  const int cus = num_cus();
+  *plan = fls::attention_plan(s->q_rows, (uint32_t)s->sequences, (uint32_t)s->heads, (uint32_t)s->kv_heads, (uint32_t)s->head_dim, max_q, max_k,
+                              cus > 0 ? (uint32_t)cus : 256u);  // without a GPU nothing is launched, but sizes can be asked for
   return plan->units <= (plan->few ? (1ull << 29) - 1 : (1ull << 24) - 8) && (plan->chunks == 1 || plan->part_rows * s->heads < (1ull << 24));
 }
 
@@ -694,6 +696,17 @@ void fls_internal_fp8_plan(uint32_t M, uint32_t K, uint32_t N, int cus, uint32_t
   out[1] = plan.tile_m;
   out[2] = plan.tile_n;
   out[3] = plan.slices;
+}
+
+void fls_internal_attention_plan(int64_t q_rows, int32_t sequences, int32_t heads, int32_t kv_heads, int32_t head_dim, int64_t max_q, int64_t max_k, int cus, uint32_t* out) {
+  const fls::AttentionPlan plan =
+      fls::attention_plan(q_rows, (uint32_t)sequences, (uint32_t)heads, (uint32_t)kv_heads, (uint32_t)head_dim, max_q, max_k, (uint32_t)cus);
+  out[0] = plan.few;
+  out[1] = plan.chunk;
+  out[2] = plan.chunks;
+  out[3] = (uint32_t)plan.units;
+  out[4] = plan.waves;
+  out[5] = plan.tile;
 }
 
 void fls_internal_shares(uint32_t M, uint32_t K, int cus, float tile_us, int wide, uint32_t* out) {

@@ -655,17 +655,18 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p) 
 
 static uint32_t padded_dim(uint32_t dim) { return dim <= 64 ? 64 : dim <= 96 ? 96 : 128; }
 
-// Chunks for many queries, by an estimate (us) that takes all sequences to have max_k keys.  `busy` workgroups of 128 queries, two to a CU: a tile of 64 keys takes
+// Chunks for many queries, by an estimate (us) that takes all sequences to have max_k keys.  `busy` workgroups of 128 queries, two to a CU: on 256 CUs a tile of 64 keys takes
 // 1.15 us where half of the CUs have one, 1.6 one on each, 2.2 two on each (of 96 values 0.86 of that, of 64 0.73); sums are written and read, and a second kernel is
-// started.  512 queries, 64 heads of 128, in front of 512, 2512 and 8512 keys, one chunk and two: 21 and 29, 72 and 66, 216 and 163 us; 32 heads and 8512 keys
+// started.  Fewer CUs take their share of it.  512 queries, 64 heads of 128, in front of 512, 2512 and 8512 keys, one chunk and two: 21 and 29, 72 and 66, 216 and 163 us; 32 heads and 8512 keys
 // in one, two, four and eight: 153, 129, 91, 105.
-static uint32_t chunks_of_many(uint64_t busy, uint64_t part_rows_heads, uint32_t DP, uint64_t max_k, uint64_t most) {
+static uint32_t chunks_of_many(uint64_t busy, uint64_t part_rows_heads, uint32_t DP, uint64_t max_k, uint64_t most, uint32_t cus) {
   uint32_t best = 1;
   float least = 3e38f;
-  for (uint32_t c = 1; c == 1 || (c <= most && c * busy <= 1024); c += 1 + c / 8) {
-    const float units = (float)(c * busy), tiles = (float)((max_k + 64 * c - 1) / (64 * c));
+  const float share = 256.f / (float)cus;
+  for (uint32_t c = 1; c == 1 || (c <= most && c * busy <= 4u * cus); c += 1 + c / 8) {
+    const float units = (float)(c * busy) * share, tiles = (float)((max_k + 64 * c - 1) / (64 * c));
     const float tile = (0.45f + 0.0043f * DP) * (units <= 128.f ? 1.15f : units <= 256.f ? 1.15f + (units - 128.f) * 0.0036f : units <= 512.f ? 1.6f + (units - 256.f) * 0.0023f : units * 0.0043f);
-    const float us = tiles * tile + (c == 1 ? 0.f : 3.f + (float)part_rows_heads * c * DP * (8.f / 4.5e6f));
+    const float us = tiles * tile + (c == 1 ? 0.f : 3.f + (float)part_rows_heads * c * DP * (8.f / 4.5e6f) * share);
     if (us < least) {
       least = us;
       best = c;
@@ -674,7 +675,7 @@ static uint32_t chunks_of_many(uint64_t busy, uint64_t part_rows_heads, uint32_t
   return best;
 }
 
-AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads, uint32_t kv_heads, uint32_t dim, int64_t max_q, int64_t max_k) {
+AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads, uint32_t kv_heads, uint32_t dim, int64_t max_q, int64_t max_k, uint32_t cus) {
   AttentionPlan plan = {};
   const uint32_t rep = heads / kv_heads;
   const uint64_t packed = (uint64_t)max_q * rep, row_blocks = (packed + 31) / 32;  // rows of queries that share keys
@@ -686,7 +687,7 @@ AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads,
   // workgroups with work if the keys are not split: about.  With few queries one to a CU is enough (4 sequences of 8000 keys, 8 key heads: 256 of them 30 us, 512 34, 1024 38).
   // A chunk has 256 keys at least (1 token behind 1000 keys, 8 key heads: 12.1 us in a graph, 14.6 with 512, 11.6 with 128; behind 4000: 14.3, 15.9, 15.3).
   const uint64_t busy = plan.few ? (uint64_t)sequences * kv_heads * plan.row_blocks : ((uint64_t)q_rows + kTileQ - 1) / kTileQ * heads;
-  const uint64_t most = ((uint64_t)max_k + 255) / 256, wanted = plan.few ? 256u / (busy ? busy : 1) : chunks_of_many(busy, q_rows * heads, padded_dim(dim), max_k, most);
+  const uint64_t most = ((uint64_t)max_k + 255) / 256, wanted = plan.few ? cus / (busy ? busy : 1) : chunks_of_many(busy, q_rows * heads, padded_dim(dim), max_k, most, cus);
   uint64_t chunks = wanted < most ? wanted : most;
   if (chunks < 1) chunks = 1;
   plan.chunk = (uint32_t)((((uint64_t)max_k + chunks - 1) / chunks + 127) / 128 * 128);
@@ -697,17 +698,19 @@ AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads,
   plan.parts_bytes = plan.chunks > 1 ? plan.part_rows * heads * plan.chunks * (padded_dim(dim) + 2) * sizeof(float) : 0;
   plan.slots = (uint32_t)(q_rows / kTileQ) + sequences;
   plan.units = (plan.few ? busy : (uint64_t)plan.slots * heads) * plan.chunks;
+  // Four waves to a workgroup where every CU has one at most (8 key heads, 1000 keys: 11.9 us, 13.1 with two), else two (16 such sequences: 19.9 us, 26.4 with four)
+  plan.waves = !plan.few || plan.units <= cus ? 4u : 2u;
+  // Tiles of 32 keys where heads have 128 values and there are more than four workgroups to a CU, none of them long: 8 prompts of 1024, 56 heads, 181 us, 196 with 64; 16 of 512 123 and 129; 4 of
+  // 2048 303 and 308; 2 of 4096 553 and 549; one of 8192 1050 and 1035; 512 queries behind 2000 keys, 64 heads (512 workgroups) 77 and 63.
+  plan.tile = plan.few || (padded_dim(dim) == 128u && plan.units > 4u * cus && max_k <= 2048) ? 32u : 64u;
   return plan;
 }
 
 template <int DP>
 static hipError_t run(AttentionParams& p, const AttentionPlan& plan, hipStream_t stream) {
-  // Four waves to a workgroup where every CU has one at most (8 key heads, 1000 keys: 11.9 us, 13.1 with two), else two (16 such sequences: 19.9 us, 26.4 with four)
-  if (plan.few && p.units <= 256u) attention_few_kernel<DP, 4><<<p.units, 256, 0, stream>>>(p);
+  if (plan.few && plan.waves == 4u) attention_few_kernel<DP, 4><<<p.units, 256, 0, stream>>>(p);
   else if (plan.few) attention_few_kernel<DP, 2><<<dim3(min(p.units, kGridRow), (p.units + kGridRow - 1u) / kGridRow), 128, 0, stream>>>(p);
-  // Tiles of 32 keys where heads have 128 values and there are more than four workgroups to a CU, none of them long: 8 prompts of 1024, 56 heads, 181 us, 196 with 64; 16 of 512 123 and 129; 4 of
-  // 2048 303 and 308; 2 of 4096 553 and 549; one of 8192 1050 and 1035; 512 queries behind 2000 keys, 64 heads (512 workgroups) 77 and 63.
-  else if (DP == 128 && p.units > 1024u && p.max_k <= 2048u) attention_kernel<DP, DP == 128 ? 32 : 64><<<(p.units + 7u) / 8u * 8u, 256, 0, stream>>>(p);
+  else if (DP == 128 && plan.tile == 32u) attention_kernel<DP, DP == 128 ? 32 : 64><<<(p.units + 7u) / 8u * 8u, 256, 0, stream>>>(p);
   else attention_kernel<DP, 64><<<(p.units + 7u) / 8u * 8u, 256, 0, stream>>>(p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.chunks == 1u) return e;

@@ -452,8 +452,10 @@ struct AttentionPlan {
   uint64_t part_rows;  // rows of sums to a chunk, each with all heads
   size_t parts_bytes;
   uint64_t units;      // workgroups, also those with no work
+  uint32_t waves;      // to a workgroup
+  uint32_t tile;       // keys to a tile
 };
-AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads, uint32_t kv_heads, uint32_t dim, int64_t max_q, int64_t max_k);
+AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads, uint32_t kv_heads, uint32_t dim, int64_t max_q, int64_t max_k, uint32_t cus);
 hipError_t launch_attention(const AttentionLaunch& a, const AttentionPlan& plan, hipStream_t stream);
 
 }  // namespace fls
@@ -469,6 +471,9 @@ extern "C" void fls_internal_dense_plan(uint32_t M, uint32_t K, uint32_t N, int 
 
 // What fls_fp8_gemm runs: out = pass (0: streamed, X quantised on the way, 1: streamed, 2: tiles), tile_m, tile_n, slices of Fp8Plan.  As above.
 extern "C" void fls_internal_fp8_plan(uint32_t M, uint32_t K, uint32_t N, int cus, uint32_t* out);
+
+// How fls_attention cuts a call of that shape (its sizes only) on a GPU of `cus` CUs: out = few, chunk, chunks, units, waves, tile of AttentionPlan.  As above.
+extern "C" void fls_internal_attention_plan(int64_t q_rows, int32_t sequences, int32_t heads, int32_t kv_heads, int32_t head_dim, int64_t max_q, int64_t max_k, int cus, uint32_t* out);
 
 // How the tiles of an M x K matrix are shared out in the passes of up to 32 columns: out = P, unit, grid of Shares.  As above.
 extern "C" uint32_t fls_internal_divide(uint32_t n, uint32_t d);  // as the kernels divide
