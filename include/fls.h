@@ -319,8 +319,9 @@ size_t fls_attention_workspace_bytes(const fls_attention_shape* shape_host);
  * those up to there.  Keys that a query does not see do not touch it, be they infinite or NaN.  O may not overlap Q, K or V.
  * The same call gives the same bits every time.  Nothing is launched, and no pointer looked at, where there is no query (sequences, q_rows or max_q is 0);
  * K_dev and V_dev may be null where k_rows is 0.
- * max_q decides how the work is cut: for few queries (32, or 16 where four and more heads share a key head) keys and values are read once for 32 rows of all these
- * heads; beyond, a workgroup takes 128 queries of a head.  Single tokens beside prompts of many are faster in a call of their own.
+ * max_q and max_k decide how the work is cut.  Few queries - max_q x r at most 32, r = heads / kv_heads; or r at least 4, max_k over 512, and max_q x r at most
+ * 32 x (r / 2, rounded down), which is max_q up to 16 for an even r: keys and values are read once for 32 rows of all heads that share them; beyond, a workgroup
+ * takes 128 queries of a head.  (max_q and max_k count as q_rows and k_rows at most.)  Single tokens beside prompts of many are faster in a call of their own.
  * Errors: FLS_EINVAL (also for work in more than 2^24 - 8 workgroups of 128 queries, or 2^29 of few), FLS_EALIGN, FLS_EWORKSPACE, FLS_EHIP.
  */
 int fls_attention(const void* Q_dev, const void* K_dev, const void* V_dev, void* O_dev, float* lse_dev, const int32_t* q_start_dev,

@@ -12,7 +12,6 @@
 namespace fls {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef float float16v __attribute__((ext_vector_type(16)));
 
 constexpr uint32_t kBlock = 128;             // k that share a scale = K of one MFMA
 constexpr uint32_t kPanel = 4;               // tile columns of a panel

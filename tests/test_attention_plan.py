@@ -53,3 +53,14 @@ def test_chunks_of_many_queries_as_measured(plan):
     for heads, max_k in ((64, 1024), (64, 9024), (32, 9024), (16, 30000)):
         for less in (2, 4, 8):
             assert chunks(heads // less, max_k, 256 // less) == chunks(heads, max_k)
+
+
+@pytest.mark.parametrize("rep", [1, 2, 3, 4, 5, 8, 13, 64])
+def test_what_counts_as_few_queries(plan, rep):
+    """As the header says: max_q x r <= 32; or r >= 4, max_k > 512 and max_q x r <= 32 (r / 2)."""
+    few = lambda max_q, max_k, rows=1 << 20: plan(rows, 3, 2 * rep, 2, 64, max_q, max_k)["few"]  # noqa: E731
+    for max_q in range(1, 70):
+        assert few(max_q, 512) == (max_q * rep <= 32)
+        assert few(max_q, 513) == (max_q * rep <= 32 or (rep >= 4 and max_q * rep <= 32 * (rep // 2)))
+    most = max(q for q in range(1, 70) if few(q, 513))
+    assert most == {1: 32, 2: 16, 3: 10, 4: 16, 5: 12, 8: 16, 13: 14, 64: 16}[rep]
