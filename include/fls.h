@@ -295,11 +295,11 @@ int fls_fp8_gemm(const void* Wq_dev, const void* Ws_dev, const void* X_dev, void
  */
 typedef struct {
   int64_t q_rows;              /* rows of Q, O and of each head of lse */
-  int64_t k_rows;              /* rows of K and V, less than 2^31, as q_rows */
-  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head; /* strides: multiples of 8, rows of at most 2^22 */
-  int32_t sequences, heads, kv_heads; /* kv_heads divides heads */
+  int64_t k_rows;              /* rows of K and V, less than 2^31 - 1, as q_rows */
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head; /* strides: multiples of 8, rows' at most 2^22, heads' 2^40 */
+  int32_t sequences, heads, kv_heads; /* at most 2^24 sequences and 65536 heads; kv_heads divides heads */
   int32_t head_dim;            /* a multiple of 8, at most FLS_MAX_HEAD_DIM */
-  int64_t max_q, max_k;        /* no sequence has more queries or keys; one that does counts as cut to its first so many */
+  int64_t max_q, max_k;        /* no sequence has more queries or keys; one that does counts as cut to its first so many; max_q under 2^31 - 1, max_k under 2^31 - 4097 */
   float scale;                 /* positive, at most 2e38 */
 } fls_attention_shape;
 
@@ -316,7 +316,8 @@ size_t fls_attention_workspace_bytes(const fls_attention_shape* shape_host);
  * Uses the registered workspace; enqueues kernels only, so it may be recorded into a HIP graph and replayed with other lengths, as long as
  * max_q and max_k hold.  The lengths are read on the device, and what lies outside the tensors is neither read nor written: a sequence whose
  * queries are not all inside 0 ... q_rows has none, one whose k_start is outside 0 ... k_rows has no keys, one whose keys reach beyond k_rows has
- * those up to there.  Keys that a query does not see do not touch it, be they infinite or NaN.  O may not overlap Q, K or V.
+ * those up to there.  Keys that a query does not see do not touch it, be they infinite or NaN.  O may not overlap Q, K or V, and its strides have to give every value a
+ * place of its own (heads beside each other in a row, or rows beside each other in a head).
  * The same call gives the same bits every time.  Nothing is launched, and no pointer looked at, where there is no query (sequences, q_rows or max_q is 0);
  * K_dev and V_dev may be null where k_rows is 0.
  * max_q and max_k decide how the work is cut.  Few queries - max_q x r at most 32, r = heads / kv_heads; or r at least 4, max_k over 512, and max_q x r at most

@@ -86,3 +86,15 @@ def test_the_binding_refuses_what_is_not_on_the_gpu(fls):
         fls.fls_attention(Q, Q, Q, Q, torch.zeros(2, dtype=torch.int32), n, n, 1, 1, 1.0)
     with pytest.raises(AssertionError):
         fls.fls_quantize(Q[0])
+
+
+def test_the_limits_that_the_header_names(fls):
+    """The last that is taken, the first that is not."""
+    size = lambda **c: fls.lib().fls_attention_workspace_bytes(shape(fls, **c))  # noqa: E731
+    big = (1 << 31) - 1
+    for last, step, rest in ((("k_rows", big - 1), 1, {}), (("q_rows", big - 1), 1, dict(max_q=1)), (("max_q", big - 1), 1, {}), (("max_k", (1 << 31) - 4098), 1, {}),
+                             (("sequences", 1 << 24), 1, dict(heads=1, kv_heads=1, max_q=1)), (("heads", 65536), 2, dict(q_rows=1, max_q=1)), (("k_row", 1 << 22), 8, {}),
+                             (("v_head", 1 << 40), 8, {}), (("head_dim", 128), 8, dict(o_head=128, o_row=1024)), (("scale", 2e38), 1e37, {})):
+        name, value = last
+        assert size(**{**rest, name: value}) > 0, name
+        assert size(**{**rest, name: value + step}) == 0, name
