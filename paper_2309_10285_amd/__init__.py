@@ -435,6 +435,13 @@ def _on_this_device(*tensors):
     return all(t.get_device() == device for t in tensors)
 
 
+def _check_devices(*tensors):
+    """That, and the workspace's: there is one."""
+    assert _on_this_device(*tensors)
+    if _ws_tensor is not None and not _on_this_device(_ws_tensor):
+        raise FlsError(EWORKSPACE, "the workspace is another device's")
+
+
 def ensure_fp8_workspace(M, K, N):
     """ensure_workspace for fls_fp8_gemm; not while a graph is recorded, unless it is large enough already."""
     need = lib().fls_fp8_workspace_bytes(M, K, N)
@@ -450,7 +457,8 @@ def _fp8_args(Wq, Ws, X, C, M, K, N):
     assert X.is_cuda and X.dtype == torch.float16 and X.is_contiguous() and X.shape == (N, K)
     assert C.is_cuda and C.dtype == torch.float16 and C.is_contiguous() and C.shape == (N, M)
     stream = _stream()
-    assert not _several_devices or _on_this_device(Wq, Ws, X, C)
+    if _several_devices:
+        _check_devices(Wq, Ws, X, C)
     return Wq.data_ptr(), Ws.data_ptr(), X.data_ptr(), C.data_ptr(), M, K, N, stream
 
 
@@ -510,7 +518,8 @@ def _attention_args(Q, K, V, O, q_start, k_start, k_len, max_q, max_k, scale, ls
     if lse is not None:
         assert lse.is_cuda and lse.dtype == torch.float32 and lse.shape == (heads, q_rows) and lse.is_contiguous()
     stream = _stream()
-    assert not _several_devices or _on_this_device(Q, K, V, O, q_start, k_start, k_len, Q if lse is None else lse)
+    if _several_devices:
+        _check_devices(Q, K, V, O, q_start, k_start, k_len, Q if lse is None else lse)
     if q_rows <= 1:  # the stride of one row or one head says nothing
         q0 = o0 = 0
     if k_rows <= 1:

@@ -88,3 +88,55 @@ def test_in_turn_with_a_callers_own_workspace(fls):
         fls.ensure_fp8_workspace(1024, 1024, 8)
         assert fls._ws_tensor.numel() > small.numel()
     assert len(fls._ws_made) == 2
+
+
+@pytest.mark.parametrize("operator", ["fp8", "attention"])
+@pytest.mark.parametrize("prepared", [False, True])
+def test_a_workspace_on_another_device_is_refused(monkeypatch, operator, prepared):
+    """There is one workspace; a call on a second GPU must not write its sums into the first one's memory.  Host tensors, as far as the binding can tell on the current GPU."""
+    import torch
+
+    import paper_2309_10285_amd as f
+
+    launched = []
+
+    class Library:
+        def fls_fp8_gemm(self, *args):
+            launched.append(args)
+            return 0
+
+        fls_attention = fls_fp8_gemm
+        fls_strerror = staticmethod(lambda code: b"")
+
+    class Workspace:
+        def __init__(self, device):
+            self.device = device
+
+        def get_device(self):
+            return self.device
+
+    here = torch.zeros(1).get_device()
+    library = Library()
+    monkeypatch.setattr(f, "lib", lambda: library)
+    monkeypatch.setattr(f, "_stream", lambda: 0)
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True, raising=False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: here)
+    half = lambda *s: torch.zeros(s, dtype=torch.float16)  # noqa: E731
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
+    if operator == "fp8":
+        args = (torch.zeros(8, 128, dtype=torch.uint8).view(torch.float8_e4m3fn), torch.zeros(8, 4, dtype=torch.uint8).view(torch.float8_e8m0fnu), half(2, 128), half(2, 8), 8, 128, 2)
+        call = (lambda: f.prepare_fp8_gemm(*args)()) if prepared else lambda: f.fls_fp8_gemm(*args)
+    else:
+        args = (half(2, 2, 64), half(5, 1, 64), half(5, 1, 64), half(2, 2, 64), ints(0, 2), ints(0), ints(5), 2, 5, 1.0)
+        call = (lambda: f.prepare_attention(*args)()) if prepared else lambda: f.fls_attention(*args)
+    for several, workspace, fine in ((False, Workspace(here), True), (True, Workspace(here), True), (True, None, True), (True, Workspace(here + 1), False)):
+        monkeypatch.setattr(f, "_several_devices", several)
+        monkeypatch.setattr(f, "_ws_tensor", workspace)
+        del launched[:]
+        if fine:
+            call()
+            assert len(launched) == 1
+        else:
+            with pytest.raises(f.FlsError) as e:
+                call()
+            assert e.value.code == f.EWORKSPACE and launched == []
