@@ -552,3 +552,44 @@ def test_tensors_of_another_device_are_refused(fls, monkeypatch):
     for f in (call, product, lambda: fls.fls_quantize(W)):
         with pytest.raises(AssertionError):
             f()
+
+
+@pytest.mark.parametrize("D", [72, 80, 96])
+@pytest.mark.parametrize("nq,nk", [([1, 1], [100, 9000]), ([4, 3], [70, 6]), ([150, 64], [150, 70]), ([100], [7000]), ([3] * 150, [5 + n for n in range(150)])])
+def test_what_is_not_seen_does_not_matter_in_heads_of_up_to_96(fls, D, nq, nk):
+    """Kernels of their own: 96 values in a row of 128."""
+    test_what_is_not_seen_does_not_matter(fls, D, nq, nk)
+
+
+LOW, HIGH = -(1 << 31), (1 << 31) - 1
+
+
+@pytest.mark.parametrize("H,G,D,nq,nk", [(2, 1, 64, [2, 2, 2], [50, 60, 70]), (4, 2, 96, [1, 2, 1], [9000, 3000, 40]), (2, 2, 128, [1] * 150, [40] * 150), (2, 1, 64, [140, 150, 130], [140, 160, 170]),
+                                         (2, 1, 80, [100, 90, 160], [6000, 90, 500]), (96, 96, 128, [300, 260, 500], [300, 260, 600]), (1, 1, 128, [70] + [2] * 70 + [60], [75] + [9] * 70 + [60])],
+                         ids=["few", "few chunks", "few of two waves", "many", "many chunks", "many small tiles", "more than lanes"])
+def test_lengths_outside_the_tensors_against_the_definition(fls, H, G, D, nq, nk):
+    """A sequence whose queries are not all inside has none and its rows stay as they were; one whose keys begin outside has none, one whose keys reach past the end has those up to there."""
+    import torch
+
+    Q, K, V, q_start, k_start, k_len = case(H, G, D, nq, nk, seed=D, slack=3)
+    rows, k_rows, n, mq, mk = Q.shape[0], K.shape[0], len(nq), max(nq), max(nk) + 100
+    at = lambda values, i, x: values[:i % len(values)] + [x] + values[i % len(values) + 1:]  # noqa: E731
+    changes = [dict(k_len=at(k_len, i, x)) for i, x in ((1, -3), (0, LOW), (n - 1, 0), (n - 1, HIGH), (n - 1, nk[-1] + 90))]
+    changes += [dict(k_start=at(k_start, i, x)) for i, x in ((0, -1), (1, k_rows), (n - 1, HIGH), (1, LOW), (0, k_rows - 1), (n - 1, k_rows - 5))]
+    changes += [dict(k_start=at(k_start, 1, HIGH), k_len=at(k_len, 1, HIGH)), dict(k_start=[-1] * n)]
+    changes += [dict(q_start=q) for q in (at(q_start, 0, -5), at(q_start, 0, LOW), [-7, -2] + q_start[2:], at(q_start, n, rows + 1), at(q_start, n, HIGH), q_start[:2] + [1 << 30] * (n - 1),
+                                          q_start[:2] + [rows] * (n - 1) if q_start[1] + mq >= rows else q_start[:2] + [q_start[1]] * (n - 1), [LOW] * n + [HIGH], [rows] * (n + 1), [-9] * (n + 1))]
+    for change in changes:
+        q, k, length = change.get("q_start", q_start), change.get("k_start", k_start), change.get("k_len", k_len)
+        assert all(a <= b for a, b in zip(q, q[1:]))
+        O, lse = attend(fls, Q, K, V, q, k, length, 0.1, max_q=mq, max_k=mk)
+        untouched = torch.ones(rows, dtype=torch.bool, device="cuda")
+        for b in range(n):
+            if not (0 <= q[b] < q[b + 1] <= rows):
+                continue
+            count = min(q[b + 1] - q[b], mq)
+            keys = min(length[b], k_rows - k[b], mk) if 0 <= k[b] < k_rows and length[b] > 0 else 0
+            there = slice(q[b], q[b] + count)
+            untouched[there] = False
+            check(O[there], lse[:, there].contiguous(), reference(Q[there], K, V, [0, count], [k[b] if keys else 0], [keys], 0.1))
+        assert (O[untouched] == 5).all() and (lse[:, untouched] == 5).all()
