@@ -323,7 +323,8 @@ size_t fls_attention_workspace_bytes(const fls_attention_shape* shape_host);
  * max_q and max_k decide how the work is cut.  Few queries - max_q x r at most 32, r = heads / kv_heads; or r at least 4, max_k over 512, and max_q x r at most
  * 32 x (r / 2, rounded down), which is max_q up to 16 for an even r: keys and values are read once for 32 rows of all heads that share them; beyond, a workgroup
  * takes 128 queries of a head.  (max_q and max_k count as q_rows and k_rows at most.)  Single tokens beside prompts of many are faster in a call of their own.
- * Errors: FLS_EINVAL (also for work in more than 2^24 - 8 workgroups of 128 queries, or 2^29 of few), FLS_EALIGN, FLS_EWORKSPACE, FLS_EHIP.
+ * Errors: FLS_EINVAL (also for work in more than 2^24 - 8 workgroups of 128 queries, or 2^29 of few, and where workgroups of 128 queries times sequences are more than
+ * 2^43: each of them looks through the sequences for its own, which takes longer than the work itself from some thousands of sequences on), FLS_EALIGN, FLS_EWORKSPACE, FLS_EHIP.
  */
 int fls_attention(const void* Q_dev, const void* K_dev, const void* V_dev, void* O_dev, float* lse_dev, const int32_t* q_start_dev,
                   const int32_t* k_start_dev, const int32_t* k_len_dev, const fls_attention_shape* shape_host, fls_stream_t stream);

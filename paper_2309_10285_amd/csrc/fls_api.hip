@@ -631,7 +631,10 @@ static bool attention_shape_ok(const fls_attention_shape* s, fls::AttentionPlan*
   const int cus = num_cus();
   *plan = fls::attention_plan(s->q_rows, (uint32_t)s->sequences, (uint32_t)s->heads, (uint32_t)s->kv_heads, (uint32_t)s->head_dim, max_q, max_k,
                               cus > 0 ? (uint32_t)cus : 256u);  // without a GPU nothing is launched, but sizes can be asked for
-  return plan->units <= (plan->few ? (1ull << 29) - 1 : (1ull << 24) - 8) && (plan->chunks == 1 || plan->part_rows * s->heads < (1ull << 24));
+  if (plan->units > (plan->few ? (1ull << 29) - 1 : (1ull << 24) - 8) || (plan->chunks != 1 && plan->part_rows * s->heads >= (1ull << 24))) return false;
+  // A workgroup of many queries looks for its sequence among all of them, 64 at a time: 16384 single tokens with max_q = 40, 8 heads, 5.6 ms, 0.16 ns for 64 sequences and a workgroup;
+  // at 2^43 of both some 20 s.
+  return plan->few || plan->units * (uint64_t)s->sequences <= 1ull << 43;
 }
 
 size_t fls_attention_workspace_bytes(const fls_attention_shape* shape_host) {

@@ -98,3 +98,15 @@ def test_the_limits_that_the_header_names(fls):
         name, value = last
         assert size(**{**rest, name: value}) > 0, name
         assert size(**{**rest, name: value + step}) == 0, name
+
+
+def test_a_search_without_end_is_refused(fls):
+    """With many queries a workgroup looks through the sequences for its own: workgroups times sequences are bounded, at some 20 seconds.  One query to a sequence needs no search."""
+    size = lambda **c: fls.lib().fls_attention_workspace_bytes(shape(fls, **c))  # noqa: E731
+    n = 1 << 20
+    many = dict(q_rows=n, sequences=n, max_q=100, kv_heads=1, o_row=512)
+    assert ((n // 128 + n) * 4) * n <= 1 << 43 < ((n // 128 + n) * 8) * n
+    assert size(**many, heads=4) > 0
+    assert size(**many, heads=8) == 0
+    assert size(**{**many, "sequences": n // 2}, heads=8) > 0
+    assert size(**{**many, "max_q": 1}, heads=8) > 0
