@@ -297,7 +297,7 @@ __device__ __forceinline__ float log_sum(float m, float l) { return l > 0.f ? (m
 
 // --- many queries to a sequence ------------------------------------------------------------------------------------------------
 // A workgroup has 128 queries of a head, 32 to a wave; tiles of 32 or 64 keys go through LDS in two stages.  Tiles that every query sees
-// come first, in a loop without a mask.  A prompt of 8192, 64 heads of 128 on 8: 1127 us, 0.98 PFLOP/s, bound by power (1.8 GHz; 864 us with all inputs zero).  Eight prompts of
+// come first, in a loop without a mask.  A prompt of 8192, 64 heads of 128 on 8: 1127 - 1190 us, 0.92 - 0.98 PFLOP/s, bound by power (1.8 GHz; the same cycles at 2.4 GHz, 851 us, with all inputs zero).  Eight prompts of
 // 17 - 1500, 56 heads of 128: 194 us, of which queries and results some 30: a workgroup's start and end have only the others on its CU to hide behind.  Two fit in 64 KB of LDS each and 256
 // registers; three in 32 KB and 168 registers, with rows of 64 values (8 prompts of 1024, 56 heads of 64, 119 -> 112 us, 64 of 128 63 -> 55) or tiles of 32 keys.
 
@@ -701,7 +701,7 @@ AttentionPlan attention_plan(int64_t q_rows, uint32_t sequences, uint32_t heads,
   // Four waves to a workgroup where every CU has one at most (8 key heads, 1000 keys: 11.9 us, 13.1 with two), else two (16 such sequences: 19.9 us, 26.4 with four)
   plan.waves = !plan.few || plan.units <= cus ? 4u : 2u;
   // Tiles of 32 keys where heads have 128 values and there are more than four workgroups to a CU, none of them long: 8 prompts of 1024, 56 heads, 181 us, 196 with 64; 16 of 512 123 and 129; 4 of
-  // 2048 303 and 308; 2 of 4096 553 and 549; one of 8192 1050 and 1035; 512 queries behind 2000 keys, 64 heads (512 workgroups) 77 and 63.
+  // 2048 303 and 308; 2 of 4096 553 and 549; one of 8192 1050 and 1035; 512 queries behind 2000 keys, 64 heads (512 workgroups) 77 and 63; heads of 96 lose by it (3 chunks of 100 - 700 queries, 32 heads of 80: 75 and 69).
   plan.tile = plan.few || (padded_dim(dim) == 128u && plan.units > 4u * cus && max_k <= 2048) ? 32u : 64u;
   return plan;
 }

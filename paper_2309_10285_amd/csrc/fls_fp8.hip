@@ -264,13 +264,13 @@ __global__ __launch_bounds__(stream_waves(NB) * 64) void fp8_stream_kernel(Fp8Pa
   }
 }
 
-// More columns: bound by the matrix cores (and by power), if LDS is read while they multiply.  A workgroup of eight waves has TM x TN of C, a wave TM/WM x TN/WN.
+// More columns: bound by power and by the loads (12288 x 12288, N = 4096: all inputs zero 464 us at 2.3 GHz), if LDS is read while the matrix cores multiply.  A workgroup of eight waves has TM x TN of C, a wave TM/WM x TN/WN.
 // Steps of 128 k of both operands go to LDS without passing through registers, into two stages.  The two waves of a SIMD take turns: while one takes
 // its fragments of a step into registers (phase 2 t for the first four waves, 2 t + 1 for the others), the other multiplies; barriers keep them
 // in step.  From phase 2 t + 2 on nobody reads step t in LDS, and step t + 2 is loaded in its place, two phases before it is read.  16-byte
 // piece c of a row lies at place c ^ (row & 7): eight lanes that read the same piece of eight rows read eight different places.
 // Scales come 16 steps at a time, 16 bytes to a row: a row's scales lie apart from its neighbours', so a load for every step asked the L2 for
-// half as many lines as the operands do.  12288 x 12288, N = 4096: 485 us, 2.5 PFLOP/s, matrix cores 61 % busy at 1.99 GHz.
+// half as many lines as the operands do.  12288 x 12288, N = 4096: 485 - 498 us, 2.5 PFLOP/s, matrix cores 61 % busy at 1.9 - 2.0 GHz.
 template <int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(512, 2) void fp8_tile_kernel(Fp8Params p) {
   constexpr int kThreads = 512, MT = TM / WM / 16, NT = TN / WN / 16, kRows = TM + TN;
